@@ -142,6 +142,46 @@ int tv_tree_verify_attention_paged(const void* q, const void* k_pool, const void
                                    void* workspace, size_t workspace_bytes,
                                    hipStream_t stream);
 
+/* ---- A paged cache in 8 bits ------------------------------------------
+ *
+ * Half the bytes per cached position.  Pages hold their heads one after the
+ * other, and every group of 32 consecutive positions of a page and head
+ * shares one exponent byte:
+ *
+ *   k_pool, v_pool [num_blocks, Hkv, block_size, D]       e4m3 codes (OCP)
+ *   k_exp, v_exp   [num_blocks, Hkv, block_size / 32]     bytes e (E8M0)
+ *
+ * A code c of a group with exponent byte e stands for c * 2^(e - 127).  The
+ * writers below use e in [16, 247]; readers take any e in [1, 247] whose
+ * values are normal bf16 numbers or zero (smaller ones may be read as zero).
+ * Position t of sequence b is row t % block_size of page
+ * block_table[b, t / block_size], as in the bf16 paged cache.  block_size is
+ * a power of two in [32, 2^20], max_blocks * block_size <= 2^30, and
+ * num_blocks * Hkv * block_size / 32 < 2^31 (TV_ERR_UNSUPPORTED above).
+ */
+
+/*
+ * tv_tree_verify_attention over such a cache.  The tree's own keys and
+ * values are bf16 and separate (k_tree, v_tree [B, N, Hkv, D], required: there
+ * is no tree-tail layout here); parent may be NULL, which stands for a chain
+ * (every node's parent is the one before it), so N = 1 with NULL is
+ * single-token decoding.  Codes enter the products as the exact bf16 values
+ * they stand for; everything else is as in tv_tree_verify_attention_paged,
+ * block table clamping included.  Codes of visible positions must not be NaN
+ * (0x7F, 0xFF).  Rows at or behind kv_len are never used, whatever they hold.
+ * The workspace is tv_tree_verify_attention_paged_fp8_workspace(B, N, Hq,
+ * Hkv, D, max_blocks * block_size) bytes, zero-filled before first use.
+ */
+size_t tv_tree_verify_attention_paged_fp8_workspace(int B, int N, int Hq, int Hkv, int D, int Lmax);
+int tv_tree_verify_attention_paged_fp8(const void* q, const void* k_pool, const void* v_pool,
+                                       const uint8_t* k_exp, const uint8_t* v_exp,
+                                       const int32_t* block_table, int block_size, int max_blocks,
+                                       int num_blocks, const void* k_tree, const void* v_tree,
+                                       const int32_t* parent, const int32_t* kv_len, void* out,
+                                       int B, int N, int Hq, int Hkv, int D, float scale,
+                                       void* workspace, size_t workspace_bytes,
+                                       hipStream_t stream);
+
 /*
  * Attention under the draft head's training mask (App. "Training Details"):
  * each of the A sampled anchors of a training example starts a block of S

@@ -25,6 +25,8 @@ Contents
   block_causal    -- attention under the draft head's training mask: anchor
                      blocks that see the prefix before their anchor and
                      their own earlier positions (App. Training Details).
+  kv_fp8          -- the paged cache in 8 bits: its codes and exponents, what its
+                     writers store, and the numbers a cache stands for.
   brute           -- pure-Python loop versions for tiny inputs, used only to
                      pin the functions above.
 
@@ -38,9 +40,10 @@ from .tree_build import draft_topw, build_tree
 from .tree_accept_sampled import tree_accept_sampled
 from .block_causal import training_mask, block_causal_attention
 from .kv_commit import commit_path, gather_paged, commit_path_paged, tree_tail, commit_path_tail
+from . import kv_fp8
 
 __all__ = ["decode_bf16", "tree_structure", "full_mask", "tree_attention",
            "target_argmax", "tree_accept", "draft_topw", "build_tree",
            "commit_path", "gather_paged", "commit_path_paged", "tree_tail",
            "commit_path_tail", "training_mask", "block_causal_attention",
-           "tree_accept_sampled"]
+           "tree_accept_sampled", "kv_fp8"]

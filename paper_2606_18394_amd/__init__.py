@@ -8,7 +8,8 @@ and raises if it is missing.  The public calls are those of ``binding``.
 
 __all__ = ["tree_verify_attention", "tree_verify_attention_paged", "tree_accept",
            "tree_accept_noalloc", "commit_path", "commit_path_paged", "draft_topw",
-           "build_tree", "block_causal_attention", "tree_accept_sampled", "load_library"]
+           "build_tree", "block_causal_attention", "tree_accept_sampled",
+           "tree_verify_attention_paged_fp8", "load_library"]
 
 
 def __getattr__(name):

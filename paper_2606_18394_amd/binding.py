@@ -19,6 +19,7 @@ LIB_PATH = os.path.join(_HERE, "libtreeverify.so")
 
 TV_BF16, TV_F32 = 0, 1
 MAX_NODES = 2048
+GROUP = 32  # positions of the 8-bit cache that share an exponent
 
 _lib = None
 _lock = threading.Lock()
@@ -64,6 +65,12 @@ def load_library() -> ctypes.CDLL:
         lib.tv_tree_verify_attention_paged.restype = ci
         lib.tv_tree_verify_attention_paged.argtypes = (
             [vp, vp, vp, i32p] + [ci] * 3 + [vp, vp, i32p, i32p, vp] + [ci] * 5
+            + [ctypes.c_float, vp, sz, vp])
+        lib.tv_tree_verify_attention_paged_fp8_workspace.restype = sz
+        lib.tv_tree_verify_attention_paged_fp8_workspace.argtypes = [ci] * 6
+        lib.tv_tree_verify_attention_paged_fp8.restype = ci
+        lib.tv_tree_verify_attention_paged_fp8.argtypes = (
+            [vp] * 5 + [i32p] + [ci] * 3 + [vp, vp, i32p, i32p, vp] + [ci] * 5
             + [ctypes.c_float, vp, sz, vp])
         lib.tv_block_causal_attention_workspace.restype = sz
         lib.tv_block_causal_attention_workspace.argtypes = [ci] * 7
@@ -248,6 +255,56 @@ def tree_verify_attention_paged(q, k_pool, v_pool, block_table, k_tree, v_tree, 
     ws = workspace_tensor if workspace_tensor is not None else workspace("attn", need, dev, stream)
     _check(lib.tv_tree_verify_attention_paged(
         _ptr(q), _ptr(k_pool), _ptr(v_pool), _ptr(block_table), bs, max_blocks, num_blocks,
+        _ptr(k_tree), _ptr(v_tree), _ptr(parent), _ptr(kv_len), _ptr(out), B, N, Hq, Hkv, D,
+        0.0 if scale is None else float(scale), _ptr(ws), ws.numel(), stream))
+    return out
+
+
+def _need_pages_fp8(k_pool, v_pool, k_exp, v_exp, block_table, B, D, dev):
+    """The 8-bit paged cache's tensors; returns its sizes."""
+    if k_pool.dim() != 4 or block_table.dim() != 2:
+        raise ValueError("k_pool must be [num_blocks, Hkv, block_size, D] and block_table "
+                         "[B, max_blocks]")
+    num_blocks, Hkv, bs, _ = k_pool.shape
+    groups = (num_blocks, Hkv, bs // GROUP)
+    _need(k_pool, "k_pool", torch.float8_e4m3fn, (num_blocks, Hkv, bs, D), dev)
+    _need(v_pool, "v_pool", torch.float8_e4m3fn, (num_blocks, Hkv, bs, D), dev)
+    _need(k_exp, "k_exp", torch.uint8, groups, dev)
+    _need(v_exp, "v_exp", torch.uint8, groups, dev)
+    _need(block_table, "block_table", torch.int32, (B, block_table.shape[1]), dev)
+    return num_blocks, Hkv, bs, block_table.shape[1]
+
+
+def tree_verify_attention_paged_fp8(q, k_pool, v_pool, k_exp, v_exp, block_table, k_tree, v_tree,
+                                    parent, out, kv_len=None, scale=None, workspace_tensor=None):
+    """tree_verify_attention over a paged cache in 8 bits: position t of
+    sequence b is row t % block_size of page block_table[b, t // block_size],
+    and a code stands for code * 2^(exp - 127), exp the byte of its page, head
+    and group of 32 positions.
+
+    k_pool/v_pool [num_blocks, Hkv, block_size, D] float8_e4m3fn (heads one
+    after the other inside a page); k_exp/v_exp [num_blocks, Hkv,
+    block_size // 32] uint8; block_table [B, max_blocks] int32; q, k_tree,
+    v_tree, out bf16 as in tree_verify_attention (no tree-tail layout);
+    parent [B, N] int32, or None for a chain (N = 1: single-token decoding).
+    """
+    lib = load_library()
+    B, N, Hq, D = q.shape
+    dev = q.device
+    _need(q, "q", torch.bfloat16, device=dev)
+    nb, Hkv, bs, mb = _need_pages_fp8(k_pool, v_pool, k_exp, v_exp, block_table, B, D, dev)
+    _need(k_tree, "k_tree", torch.bfloat16, (B, N, Hkv, D), dev)
+    _need(v_tree, "v_tree", torch.bfloat16, (B, N, Hkv, D), dev)
+    _need(out, "out", torch.bfloat16, (B, N, Hq, D), dev)
+    if parent is not None:
+        _need(parent, "parent", torch.int32, (B, N), dev)
+    if kv_len is not None:
+        _need(kv_len, "kv_len", torch.int32, (B,), dev)
+    stream = _stream(dev)
+    need = _bytes("tv_tree_verify_attention_paged_fp8_workspace", B, N, Hq, Hkv, D, mb * bs)
+    ws = workspace_tensor if workspace_tensor is not None else workspace("attn", need, dev, stream)
+    _check(lib.tv_tree_verify_attention_paged_fp8(
+        _ptr(q), _ptr(k_pool), _ptr(v_pool), _ptr(k_exp), _ptr(v_exp), _ptr(block_table), bs, mb, nb,
         _ptr(k_tree), _ptr(v_tree), _ptr(parent), _ptr(kv_len), _ptr(out), B, N, Hq, Hkv, D,
         0.0 if scale is None else float(scale), _ptr(ws), ws.numel(), stream))
     return out

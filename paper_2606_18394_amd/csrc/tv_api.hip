@@ -10,6 +10,7 @@
 
 #include "treeverify.h"
 #include "tv_plan.h"
+#include "tv_plan_fp8.h"
 
 static_assert(TV_MAX_NODES == tv::kMaxNodes, "node limit mismatch");
 static_assert(TV_MAX_DRAFT_DEPTH == tv::kMaxDraftDepth, "draft depth limit");
@@ -21,6 +22,12 @@ hipError_t launch_attention(const void* q, const void* kc, const void* vc, const
                             float scale, void* ws, const AttnPlan& p, hipStream_t st,
                             const int32_t* block_table, int block_shift, int max_blocks,
                             int num_blocks, int cgroup);
+hipError_t launch_attention_fp8(const void* q, const void* kp, const void* vp, const uint8_t* ke,
+                                const uint8_t* ve, const int32_t* block_table, int block_shift,
+                                int max_blocks, int num_blocks, const void* kt, const void* vt,
+                                const int32_t* parent, const int32_t* kv_len, void* out, int B, int N,
+                                int Hq, int Hkv, int D, int Lmax, float scale, void* ws,
+                                const AttnPlan& p, hipStream_t st);
 hipError_t launch_packed(const void* q, const void* kc, const void* vc, const void* kt, const void* vt,
                          const int32_t* anchors, void* out, int B, int A, int S, int Hq, int Hkv, int D,
                          int L, float scale, void* ws, const PackPlan& p, hipStream_t st);
@@ -242,6 +249,48 @@ int tv_tree_verify_attention_paged(const void* q, const void* k_pool, const void
                                       N, Hq, Hkv, D, Lmax, scale, workspace, p, stream,
                                       Lmax > 0 ? block_table : nullptr, shift, max_blocks,
                                       num_blocks, 1);
+  return e == hipSuccess ? TV_OK : TV_ERR_LAUNCH;
+}
+
+// The paged 8-bit cache: page sizes, and groups whose numbers stay in int32.
+static int check_pages_fp8(int Hkv, int block_size, int max_blocks, int num_blocks) {
+  if (block_shift(block_size) < 0 || max_blocks < 0 || num_blocks < 0 || Hkv < 1) return TV_ERR_SHAPE;
+  if ((long long)max_blocks * block_size > (1ll << 30)) return TV_ERR_UNSUPPORTED;
+  if ((long long)num_blocks * Hkv > ((1ll << 31) - 1) / (block_size / 32)) return TV_ERR_UNSUPPORTED;
+  return TV_OK;
+}
+
+size_t tv_tree_verify_attention_paged_fp8_workspace(int B, int N, int Hq, int Hkv, int D, int Lmax) {
+  if (check_attention_sizes(B, N, Hq, Hkv, D, Lmax) != TV_OK) return 0;
+  const size_t need = tv::attn_plan_fp8(B, N, Hq, Hkv, D, Lmax).ws_bytes;
+  return need > 0 ? need : 256;
+}
+
+int tv_tree_verify_attention_paged_fp8(const void* q, const void* k_pool, const void* v_pool,
+                                       const uint8_t* k_exp, const uint8_t* v_exp,
+                                       const int32_t* block_table, int block_size, int max_blocks,
+                                       int num_blocks, const void* k_tree, const void* v_tree,
+                                       const int32_t* parent, const int32_t* kv_len, void* out,
+                                       int B, int N, int Hq, int Hkv, int D, float scale,
+                                       void* workspace, size_t workspace_bytes,
+                                       hipStream_t stream) {
+  int rc = check_pages_fp8(Hkv, block_size, max_blocks, num_blocks);
+  if (rc != TV_OK) return rc;
+  const int Lmax = max_blocks * block_size;
+  if ((rc = check_attention_sizes(B, N, Hq, Hkv, D, Lmax)) != TV_OK) return rc;
+  if (!q || !out || !k_tree || !v_tree) return TV_ERR_NULL;
+  if (Lmax > 0 && (!k_pool || !v_pool || !k_exp || !v_exp || !block_table || num_blocks < 1))
+    return TV_ERR_NULL;
+  if (misaligned(q) || misaligned(out) || misaligned(k_tree) || misaligned(v_tree) ||
+      (Lmax > 0 && (misaligned(k_pool) || misaligned(v_pool))))
+    return TV_ERR_ALIGN;
+  const tv::AttnPlan p = tv::attn_plan_fp8(B, N, Hq, Hkv, D, Lmax);
+  if (p.ws_bytes > 0 && (!workspace || workspace_bytes < p.ws_bytes)) return TV_ERR_WORKSPACE;
+  if (misaligned(workspace)) return TV_ERR_ALIGN;
+  if (!(scale > 0.f)) scale = 1.0f / sqrtf((float)D);
+  const hipError_t e = tv::launch_attention_fp8(
+      q, k_pool, v_pool, k_exp, v_exp, block_table, block_shift(block_size), max_blocks, num_blocks,
+      k_tree, v_tree, parent, kv_len, out, B, N, Hq, Hkv, D, Lmax, scale, workspace, p, stream);
   return e == hipSuccess ? TV_OK : TV_ERR_LAUNCH;
 }
 

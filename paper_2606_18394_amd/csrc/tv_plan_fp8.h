@@ -1,0 +1,66 @@
+// Host-side launch planning of the attention over the 8-bit paged cache.  Pure C++
+// (no HIP), like tv_plan.h whose work decomposition it uses.
+#pragma once
+#include "tv_plan.h"
+
+namespace tv {
+
+// WR x WK waves; units of a key group's ring (8 KB at D = 128, 4 KB at D = 64): 64 KB for
+// every four waves, more does not fit
+constexpr Arrangement kArrangementsFp8[] = {
+    {8, 1, 8, 16}, {4, 2, 8, 16}, {2, 4, 4, 8}, {1, 8, 2, 4}, {4, 1, 8, 16},
+};
+constexpr int kNumArrangementsFp8 = sizeof(kArrangementsFp8) / sizeof(kArrangementsFp8[0]);
+
+inline AttnPlan attn_plan_fp8_arr(int B, int N, int Hq, int Hkv, int D, int Lmax, int arr, long long want) {
+  const Arrangement& ar = kArrangementsFp8[arr];
+  AttnPlan p{};
+  p.arr = arr;
+  p.WR = ar.WR;
+  p.WK = ar.WK;
+  p.NS = arr_stages(ar, D);
+  p.threads = 64 * ar.WR * ar.WK;
+  p.G = Hq / Hkv;
+  p.wg_per_cu = kWavesPerCU / (ar.WR * ar.WK);
+  p.M = N * p.G;
+  p.RB = kRowsPerWave * ar.WR;
+  p.nRB = cdiv(p.M, p.RB);
+  // the rings (attn_lds_bytes counts stages of two units), the tree tables, or the merge
+  p.lds_bytes = attn_lds_bytes(D, ar.WR, ar.WK, p.NS / 2, p.G, N, false);
+  const int tiles = cdiv(Lmax, kKeyTile) + cdiv(N, kKeyTile);
+  const long long base = (long long)B * Hkv * p.nRB;
+  const int min_chunk = 2 * ar.WK;
+  const long long max_s = tiles / min_chunk > 1 ? tiles / min_chunk : 1;
+  long long S = (want + B - 1) / B;
+  if (S > max_s) S = max_s;
+  if (S < 1 || base > kSyncGroups || B > kEvenSequences || tiles >= kEvenTiles) S = 1;
+  p.chunk = cdiv(tiles, S);
+  p.S = cdiv(tiles, p.chunk);
+  p.nwork = (int)(base * p.S);
+  p.grid = cdiv(p.nwork, kXcds) * kXcds;
+  if (p.S > 1) {
+    p.slots = (int)(want < (long long)B * p.S ? want : (long long)B * p.S);
+    p.min_chunk = min_chunk;
+    p.even_grid = kXcds * p.nRB * cdiv((long long)p.slots * Hkv, kXcds);
+    const int DT = D / 16, NTG = p.RB / 16;
+    p.ws_sync_bytes = kSyncBytes;
+    p.ws_o_bytes = (size_t)B * Hkv * p.nRB * p.S * DT * NTG * 64 * 16;
+    p.ws_ml_bytes = (size_t)B * Hkv * p.nRB * p.S * p.RB * 8;
+  }
+  p.ws_bytes = p.ws_sync_bytes + p.ws_o_bytes + p.ws_ml_bytes;
+  p.fused = p.S > 1 && (size_t)p.S * p.RB * D * 4 <= (size_t)1024 * p.threads;
+  return p;
+}
+
+inline AttnPlan attn_plan_fp8(int B, int N, int Hq, int Hkv, int D, int Lmax) {
+  const int M = N * (Hq / Hkv);
+  int arr = M <= 32 ? 3 : (M <= 64 ? 2 : (M <= 128 ? 1 : 4));
+  if (attn_plan_fp8_arr(B, N, Hq, Hkv, D, Lmax, arr, B).lds_bytes *
+          (size_t)attn_plan_fp8_arr(B, N, Hq, Hkv, D, Lmax, arr, B).wg_per_cu > kMaxLds)
+    arr = 0;
+  const AttnPlan one = attn_plan_fp8_arr(B, N, Hq, Hkv, D, Lmax, arr, B);
+  const long long fill = 256LL * one.wg_per_cu / one.nRB / Hkv;
+  return fill > B ? attn_plan_fp8_arr(B, N, Hq, Hkv, D, Lmax, arr, fill) : one;
+}
+
+}  // namespace tv
