@@ -183,6 +183,109 @@ int tv_tree_verify_attention_paged_fp8(const void* q, const void* k_pool, const 
                                        hipStream_t stream);
 
 /*
+ * Appends rows to the 8-bit cache: rows 0 .. n_new[b] - 1 of sequence b (NULL
+ * n_new: T) go to positions kv_len[b] .. and kv_len[b] grows by n_new[b].
+ *
+ *   k_new, v_new [B, T, Hkv, D] bf16, finite where used
+ *   n_new        [B] int32, in [0, T]
+ *
+ * Per group of 32 positions that gets rows, head, and K or V, with a the
+ * largest size among its new values and e(a) the least e of [16, 247] with
+ * a <= 448 * 2^(e - 127): the exponent byte becomes e(a), or, if the group
+ * holds older rows of the sequence, the larger of e(a) and its byte so far;
+ * new codes are the nearest to x * 2^(127 - e) (ties to even), and older
+ * codes the nearest to what they stand for (so unchanged unless the byte
+ * grew).  Positions behind the last row keep what they hold.  A sequence
+ * whose n_new is outside [0, T], whose kv_len is negative, or that would pass
+ * its max_blocks pages is left unchanged (pools, exponents and kv_len).
+ * Entries of block_table are clamped into the pool.  The pages that a
+ * sequence writes to must be its own: not shared with another one, which a
+ * partly filled page after tv_fork_pages is not.
+ */
+int tv_append_paged_fp8(const void* k_new, const void* v_new, const int32_t* n_new, void* k_pool,
+                        void* v_pool, uint8_t* k_exp, uint8_t* v_exp, const int32_t* block_table,
+                        int block_size, int max_blocks, int num_blocks, int32_t* kv_len, int B, int T,
+                        int Hkv, int D, hipStream_t stream);
+
+/* tv_commit_path into the 8-bit cache: the rows path[b, 0 .. accept_len[b] - 1]
+ * of k_tree, v_tree [B, N, Hkv, D] bf16 are appended as by
+ * tv_append_paged_fp8; sequences are left unchanged where tv_commit_path
+ * leaves them (failed or too long acceptance, a node outside [0, N), no room). */
+int tv_commit_path_paged_fp8(const void* k_tree, const void* v_tree, const int32_t* path,
+                             const int32_t* accept_len, void* k_pool, void* v_pool, uint8_t* k_exp,
+                             uint8_t* v_exp, const int32_t* block_table, int block_size, int max_blocks,
+                             int num_blocks, int32_t* kv_len, int B, int N, int Hkv, int D, int Dmax,
+                             hipStream_t stream);
+
+/* ---- Pages: whose is whose --------------------------------------------
+ *
+ * For paged caches of any kind.  Beside block_table [B, max_blocks] and
+ * kv_len [B] there is ref_count [num_blocks] int32, how many rows of the
+ * table name a page; 0 is a free page.  A row's pages come first and -1
+ * follows; a row whose first entry is negative is empty.  New pages are the
+ * free ones of the lowest numbers, in the order in which they are asked for:
+ * what a call does depends on its arguments alone.  Calls on one state must
+ * be ordered (one stream).
+ *
+ * Pools are what the pages hold, e.g. K, V and exponents of every layer:
+ * n_pools <= TV_MAX_POOLS device arrays whose first axis is the page, a page
+ * of pool k being page_bytes[k] bytes (any number; whole multiples of 16 at
+ * 16-byte aligned addresses are copied fastest).  pools and page_bytes are
+ * host arrays, read during the call.  More pools take further calls of
+ * tv_copy_pages with the lists that fork and compact return.
+ */
+#define TV_MAX_POOLS 64
+#define TV_MAX_FORKS 1024
+#define TV_MAX_RESERVE 4096
+
+/* Gives every sequence pages for n_rows[b] more rows: the entries of its row
+ * from its first without a page (behind the pages of its kv_len[b] rows) up
+ * to the page of row kv_len[b] + n_rows[b] - 1.  Sequences ask in their
+ * order; one is served, ok[b] = 1, if all pages asked for up to and with it
+ * are there, else it gets none and ok[b] = 0.  n_rows[b] < 0, or more rows
+ * than max_blocks pages hold: ok[b] = 0.  B <= TV_MAX_RESERVE. */
+int tv_reserve_pages(const int32_t* n_rows, int32_t* block_table, const int32_t* kv_len,
+                     int32_t* ref_count, int32_t* ok, int B, int max_blocks, int block_size,
+                     int num_blocks, hipStream_t stream);
+
+/* Sequence dst[i] becomes a continuation of sequence src[i], for i < n <=
+ * TV_MAX_FORKS: its row names src[i]'s full pages (their counts grow) and, if
+ * src[i]'s last page is partly filled, a new page that the pools' contents of
+ * it are copied to; kv_len[dst[i]] = kv_len[src[i]].  Pages that src[i] has
+ * beyond kv_len are not shared.  ok[i] = 1, or 0 where nothing is done: src[i]
+ * or dst[i] outside [0, B), row dst[i] not empty, dst[i] named by an earlier
+ * fork, src[i] the dst of any fork, or no page left for the copy (in the order
+ * of i).  copy_src, copy_dst [n]: the pages copied, -1 where none. */
+int tv_fork_pages(const int32_t* src, const int32_t* dst, int n, int32_t* block_table, int32_t* kv_len,
+                  int32_t* ref_count, int B, int max_blocks, int block_size, int num_blocks,
+                  void* const* pools, const int64_t* page_bytes, int n_pools, int32_t* ok,
+                  int32_t* copy_src, int32_t* copy_dst, hipStream_t stream);
+
+/* Sequences seqs[0 .. n - 1] end: the counts of their pages drop, their rows
+ * become empty and their kv_len 0.  Numbers outside [0, B) and repeated ones
+ * are passed over.  n <= TV_MAX_RESERVE. */
+int tv_free_pages(const int32_t* seqs, int n, int32_t* block_table, int32_t* kv_len, int32_t* ref_count,
+                  int B, int max_blocks, int num_blocks, hipStream_t stream);
+
+/* Contents of pages src[i] are copied to pages dst[i], i < n.  Pairs with a
+ * number outside [0, num_blocks) are passed over.  No page may be named by
+ * dst twice, or by src and dst (unless as a pair of its own). */
+int tv_copy_pages(const int32_t* src, const int32_t* dst, int n, int num_blocks, void* const* pools,
+                  const int64_t* page_bytes, int n_pools, hipStream_t stream);
+
+/* Draws the live pages together: with L = n_live[0] of them, every live page
+ * with a number from L on moves into a free one below L (the highest into the
+ * lowest), contents, count and the rows that name it; afterwards pages L ..
+ * num_blocks - 1 are free.  copy_src, copy_dst [num_blocks / 2]: the moves, -1
+ * behind the last one.  kv_len plays no part.  Workspace:
+ * tv_compact_pages_workspace(num_blocks) bytes, no zero fill needed. */
+size_t tv_compact_pages_workspace(int num_blocks);
+int tv_compact_pages(int32_t* block_table, int32_t* ref_count, int B, int max_blocks, int num_blocks,
+                     void* const* pools, const int64_t* page_bytes, int n_pools, int32_t* n_live,
+                     int32_t* copy_src, int32_t* copy_dst, void* workspace, size_t workspace_bytes,
+                     hipStream_t stream);
+
+/*
  * Attention under the draft head's training mask (App. "Training Details"):
  * each of the A sampled anchors of a training example starts a block of S
  * positions (the anchor, then mask tokens).  Position j of block k attends to

@@ -27,6 +27,8 @@ Contents
                      their own earlier positions (App. Training Details).
   kv_fp8          -- the paged cache in 8 bits: its codes and exponents, what its
                      writers store, and the numbers a cache stands for.
+  pages           -- which page of a paged cache belongs to whom: reserving,
+                     forking, freeing and compacting, as loops.
   brute           -- pure-Python loop versions for tiny inputs, used only to
                      pin the functions above.
 
@@ -40,10 +42,10 @@ from .tree_build import draft_topw, build_tree
 from .tree_accept_sampled import tree_accept_sampled
 from .block_causal import training_mask, block_causal_attention
 from .kv_commit import commit_path, gather_paged, commit_path_paged, tree_tail, commit_path_tail
-from . import kv_fp8
+from . import kv_fp8, pages
 
 __all__ = ["decode_bf16", "tree_structure", "full_mask", "tree_attention",
            "target_argmax", "tree_accept", "draft_topw", "build_tree",
            "commit_path", "gather_paged", "commit_path_paged", "tree_tail",
            "commit_path_tail", "training_mask", "block_causal_attention",
-           "tree_accept_sampled", "kv_fp8"]
+           "tree_accept_sampled", "kv_fp8", "pages"]

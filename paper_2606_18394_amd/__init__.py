@@ -9,7 +9,9 @@ and raises if it is missing.  The public calls are those of ``binding``.
 __all__ = ["tree_verify_attention", "tree_verify_attention_paged", "tree_accept",
            "tree_accept_noalloc", "commit_path", "commit_path_paged", "draft_topw",
            "build_tree", "block_causal_attention", "tree_accept_sampled",
-           "tree_verify_attention_paged_fp8", "load_library"]
+           "tree_verify_attention_paged_fp8", "append_paged_fp8", "commit_path_paged_fp8",
+           "reserve_pages", "fork_pages", "free_pages", "copy_pages", "compact_pages",
+           "load_library"]
 
 
 def __getattr__(name):

@@ -72,6 +72,24 @@ def load_library() -> ctypes.CDLL:
         lib.tv_tree_verify_attention_paged_fp8.argtypes = (
             [vp] * 5 + [i32p] + [ci] * 3 + [vp, vp, i32p, i32p, vp] + [ci] * 5
             + [ctypes.c_float, vp, sz, vp])
+        lib.tv_append_paged_fp8.restype = ci
+        lib.tv_append_paged_fp8.argtypes = [vp] * 8 + [ci] * 3 + [i32p] + [ci] * 4 + [vp]
+        lib.tv_commit_path_paged_fp8.restype = ci
+        lib.tv_commit_path_paged_fp8.argtypes = [vp] * 9 + [ci] * 3 + [i32p] + [ci] * 5 + [vp]
+        lib.tv_reserve_pages.restype = ci
+        lib.tv_reserve_pages.argtypes = [i32p] * 5 + [ci] * 4 + [vp]
+        lib.tv_fork_pages.restype = ci
+        lib.tv_fork_pages.argtypes = (
+            [i32p, i32p, ci] + [i32p] * 3 + [ci] * 4 + [vp, vp, ci] + [i32p] * 3 + [vp])
+        lib.tv_free_pages.restype = ci
+        lib.tv_free_pages.argtypes = [i32p, ci] + [i32p] * 3 + [ci] * 3 + [vp]
+        lib.tv_copy_pages.restype = ci
+        lib.tv_copy_pages.argtypes = [i32p, i32p, ci, ci, vp, vp, ci, vp]
+        lib.tv_compact_pages_workspace.restype = sz
+        lib.tv_compact_pages_workspace.argtypes = [ci]
+        lib.tv_compact_pages.restype = ci
+        lib.tv_compact_pages.argtypes = (
+            [i32p, i32p] + [ci] * 3 + [vp, vp, ci] + [i32p] * 3 + [vp, sz, vp])
         lib.tv_block_causal_attention_workspace.restype = sz
         lib.tv_block_causal_attention_workspace.argtypes = [ci] * 7
         lib.tv_block_causal_attention.restype = ci
@@ -260,19 +278,19 @@ def tree_verify_attention_paged(q, k_pool, v_pool, block_table, k_tree, v_tree, 
     return out
 
 
-def _need_pages_fp8(k_pool, v_pool, k_exp, v_exp, block_table, B, D, dev):
-    """The 8-bit paged cache's tensors; returns its sizes."""
+def _need_pages_fp8(k_pool, v_pool, k_exp, v_exp, block_table, B, Hkv, D, dev):
+    """The 8-bit paged cache's tensors; returns (num_blocks, block_size, max_blocks)."""
     if k_pool.dim() != 4 or block_table.dim() != 2:
         raise ValueError("k_pool must be [num_blocks, Hkv, block_size, D] and block_table "
                          "[B, max_blocks]")
-    num_blocks, Hkv, bs, _ = k_pool.shape
-    groups = (num_blocks, Hkv, bs // GROUP)
-    _need(k_pool, "k_pool", torch.float8_e4m3fn, (num_blocks, Hkv, bs, D), dev)
-    _need(v_pool, "v_pool", torch.float8_e4m3fn, (num_blocks, Hkv, bs, D), dev)
+    nb, bs, mb = k_pool.shape[0], k_pool.shape[2], block_table.shape[1]
+    groups = (nb, Hkv, bs // GROUP)
+    _need(k_pool, "k_pool", torch.float8_e4m3fn, (nb, Hkv, bs, D), dev)
+    _need(v_pool, "v_pool", torch.float8_e4m3fn, (nb, Hkv, bs, D), dev)
     _need(k_exp, "k_exp", torch.uint8, groups, dev)
     _need(v_exp, "v_exp", torch.uint8, groups, dev)
-    _need(block_table, "block_table", torch.int32, (B, block_table.shape[1]), dev)
-    return num_blocks, Hkv, bs, block_table.shape[1]
+    _need(block_table, "block_table", torch.int32, (B, mb), dev)
+    return nb, bs, mb
 
 
 def tree_verify_attention_paged_fp8(q, k_pool, v_pool, k_exp, v_exp, block_table, k_tree, v_tree,
@@ -292,8 +310,9 @@ def tree_verify_attention_paged_fp8(q, k_pool, v_pool, k_exp, v_exp, block_table
     B, N, Hq, D = q.shape
     dev = q.device
     _need(q, "q", torch.bfloat16, device=dev)
-    nb, Hkv, bs, mb = _need_pages_fp8(k_pool, v_pool, k_exp, v_exp, block_table, B, D, dev)
+    Hkv = k_tree.shape[2]
     _need(k_tree, "k_tree", torch.bfloat16, (B, N, Hkv, D), dev)
+    nb, bs, mb = _need_pages_fp8(k_pool, v_pool, k_exp, v_exp, block_table, B, Hkv, D, dev)
     _need(v_tree, "v_tree", torch.bfloat16, (B, N, Hkv, D), dev)
     _need(out, "out", torch.bfloat16, (B, N, Hq, D), dev)
     if parent is not None:
@@ -308,6 +327,159 @@ def tree_verify_attention_paged_fp8(q, k_pool, v_pool, k_exp, v_exp, block_table
         _ptr(k_tree), _ptr(v_tree), _ptr(parent), _ptr(kv_len), _ptr(out), B, N, Hq, Hkv, D,
         0.0 if scale is None else float(scale), _ptr(ws), ws.numel(), stream))
     return out
+
+
+def append_paged_fp8(k_new, v_new, k_pool, v_pool, k_exp, v_exp, block_table, kv_len, n_new=None):
+    """Append new rows to a paged cache in 8 bits (layout as in
+    tree_verify_attention_paged_fp8) behind kv_len, and advance kv_len, in
+    place: rows 0 .. n_new[b] - 1 (n_new None: all) of k_new/v_new
+    [B,T,Hkv,D] bf16 become codes and exponents.  kv_len, n_new [B] int32.  A
+    sequence without room for its rows is left unchanged."""
+    lib = load_library()
+    B, T, Hkv, D = k_new.shape
+    dev = k_new.device
+    _need(k_new, "k_new", torch.bfloat16, (B, T, Hkv, D), dev)
+    _need(v_new, "v_new", torch.bfloat16, (B, T, Hkv, D), dev)
+    nb, bs, mb = _need_pages_fp8(k_pool, v_pool, k_exp, v_exp, block_table, B, Hkv, D, dev)
+    _need(kv_len, "kv_len", torch.int32, (B,), dev)
+    if n_new is not None:
+        _need(n_new, "n_new", torch.int32, (B,), dev)
+    _check(lib.tv_append_paged_fp8(
+        _ptr(k_new), _ptr(v_new), _ptr(n_new), _ptr(k_pool), _ptr(v_pool), _ptr(k_exp), _ptr(v_exp),
+        _ptr(block_table), bs, mb, nb, _ptr(kv_len), B, T, Hkv, D, _stream(dev)))
+
+
+def commit_path_paged_fp8(k_tree, v_tree, path, accept_len, k_pool, v_pool, k_exp, v_exp,
+                          block_table, kv_len):
+    """commit_path into a paged cache in 8 bits, in place: the accepted
+    path's rows of k_tree/v_tree [B,N,Hkv,D] bf16 are appended as by
+    append_paged_fp8.  path [B,Dmax], accept_len [B], kv_len [B] int32."""
+    lib = load_library()
+    B, N, Hkv, D = k_tree.shape
+    Dmax = path.shape[1]
+    dev = k_tree.device
+    _need(k_tree, "k_tree", torch.bfloat16, (B, N, Hkv, D), dev)
+    _need(v_tree, "v_tree", torch.bfloat16, (B, N, Hkv, D), dev)
+    _need(path, "path", torch.int32, (B, Dmax), dev)
+    _need(accept_len, "accept_len", torch.int32, (B,), dev)
+    nb, bs, mb = _need_pages_fp8(k_pool, v_pool, k_exp, v_exp, block_table, B, Hkv, D, dev)
+    _need(kv_len, "kv_len", torch.int32, (B,), dev)
+    _check(lib.tv_commit_path_paged_fp8(
+        _ptr(k_tree), _ptr(v_tree), _ptr(path), _ptr(accept_len), _ptr(k_pool), _ptr(v_pool),
+        _ptr(k_exp), _ptr(v_exp), _ptr(block_table), bs, mb, nb, _ptr(kv_len), B, N, Hkv, D, Dmax,
+        _stream(dev)))
+
+
+def _need_page_state(block_table, kv_len, ref_count):
+    """block_table [B, max_blocks], kv_len [B] (or None), ref_count [num_blocks]."""
+    if block_table.dim() != 2 or ref_count.dim() != 1:
+        raise ValueError("block_table must be [B, max_blocks] and ref_count [num_blocks]")
+    B, mb = block_table.shape
+    dev = block_table.device
+    _need(block_table, "block_table", torch.int32, device=dev)
+    _need(ref_count, "ref_count", torch.int32, device=dev)
+    if kv_len is not None:
+        _need(kv_len, "kv_len", torch.int32, (B,), dev)
+    return B, mb, ref_count.shape[0], dev
+
+
+def _pool_arrays(pools, num_blocks, dev):
+    """Addresses and page sizes of tensors [num_blocks, ...], as host arrays."""
+    n = len(pools)
+    base, size = (ctypes.c_void_p * n)(), (ctypes.c_int64 * n)()
+    for i, p in enumerate(pools):
+        if not isinstance(p, torch.Tensor):
+            raise TypeError(f"pools[{i}] must be a torch.Tensor")
+        if p.dim() < 1 or p.shape[0] != num_blocks:
+            raise ValueError(f"pools[{i}] has shape {tuple(p.shape)}, expected {num_blocks} pages")
+        _need(p, f"pools[{i}]", p.dtype, device=dev)
+        base[i] = p.data_ptr()
+        size[i] = p.numel() * p.element_size() // num_blocks if num_blocks else 0
+    return base, size, n
+
+
+def reserve_pages(n_rows, block_table, kv_len, ref_count, block_size, ok=None):
+    """Pages for n_rows[b] more rows of every sequence (int32 [B]): free pages,
+    lowest numbers first, go into the rows of block_table in the order of the
+    sequences.  Returns ok [B] int32: 0 for a sequence that got none because
+    the pages asked for up to it are not there, or because its row has no room."""
+    lib = load_library()
+    B, mb, nb, dev = _need_page_state(block_table, kv_len, ref_count)
+    _need(n_rows, "n_rows", torch.int32, (B,), dev)
+    ok = _output(ok, "ok", torch.int32, (B,), dev)
+    _check(lib.tv_reserve_pages(_ptr(n_rows), _ptr(block_table), _ptr(kv_len), _ptr(ref_count),
+                                _ptr(ok), B, mb, int(block_size), nb, _stream(dev)))
+    return ok
+
+
+def fork_pages(src, dst, block_table, kv_len, ref_count, block_size, pools=(), ok=None,
+               copy_src=None, copy_dst=None):
+    """Sequence dst[i] (an empty row) continues sequence src[i] (int32 [n]): it
+    shares src's full pages, and its last, partly filled page is copied in all
+    `pools` ([num_blocks, ...] tensors).  Returns (ok, copy_src, copy_dst) int32
+    [n]: whether the fork was made, and the pages copied (-1: none), for
+    copy_pages on further pools."""
+    lib = load_library()
+    B, mb, nb, dev = _need_page_state(block_table, kv_len, ref_count)
+    n = src.shape[0]
+    _need(src, "src", torch.int32, (n,), dev)
+    _need(dst, "dst", torch.int32, (n,), dev)
+    base, size, count = _pool_arrays(pools, nb, dev)
+    ok = _output(ok, "ok", torch.int32, (n,), dev)
+    copy_src = _output(copy_src, "copy_src", torch.int32, (n,), dev)
+    copy_dst = _output(copy_dst, "copy_dst", torch.int32, (n,), dev)
+    _check(lib.tv_fork_pages(_ptr(src), _ptr(dst), n, _ptr(block_table), _ptr(kv_len),
+                             _ptr(ref_count), B, mb, int(block_size), nb, base, size, count,
+                             _ptr(ok), _ptr(copy_src), _ptr(copy_dst), _stream(dev)))
+    return ok, copy_src, copy_dst
+
+
+def free_pages(seqs, block_table, kv_len, ref_count):
+    """Sequences seqs (int32 [n]) end: the counts of their pages drop, their
+    rows of block_table become empty (-1) and their kv_len 0."""
+    lib = load_library()
+    B, mb, nb, dev = _need_page_state(block_table, kv_len, ref_count)
+    n = seqs.shape[0]
+    _need(seqs, "seqs", torch.int32, (n,), dev)
+    _check(lib.tv_free_pages(_ptr(seqs), n, _ptr(block_table), _ptr(kv_len), _ptr(ref_count), B, mb,
+                             nb, _stream(dev)))
+
+
+def copy_pages(src, dst, pools):
+    """pools[k][dst[i]] = pools[k][src[i]] for tensors [num_blocks, ...] and
+    page numbers src, dst (int32 [n]); pairs with a negative number are passed
+    over.  No page may be copied to twice, or be both copied and copied to."""
+    lib = load_library()
+    if not pools:
+        raise ValueError("copy_pages needs at least one pool")
+    n, dev, nb = src.shape[0], src.device, pools[0].shape[0]
+    _need(src, "src", torch.int32, (n,), dev)
+    _need(dst, "dst", torch.int32, (n,), dev)
+    base, size, count = _pool_arrays(pools, nb, dev)
+    _check(lib.tv_copy_pages(_ptr(src), _ptr(dst), n, nb, base, size, count, _stream(dev)))
+
+
+def compact_pages(block_table, ref_count, pools=(), n_live=None, copy_src=None, copy_dst=None,
+                  workspace_tensor=None):
+    """Draw the live pages together at the front of the pools, in place: rows of
+    block_table, counts and contents follow.  Returns (n_live [1], copy_src,
+    copy_dst [num_blocks // 2]) int32: how many pages are live, and the moves
+    made (-1 behind the last), for copy_pages on further pools."""
+    lib = load_library()
+    B, mb, nb, dev = _need_page_state(block_table, None, ref_count)
+    base, size, count = _pool_arrays(pools, nb, dev)
+    n_live = _output(n_live, "n_live", torch.int32, (1,), dev)
+    copy_src = _output(copy_src, "copy_src", torch.int32, (nb // 2,), dev)
+    copy_dst = _output(copy_dst, "copy_dst", torch.int32, (nb // 2,), dev)
+    stream = _stream(dev)
+    need = _bytes("tv_compact_pages_workspace", nb)
+    ws = workspace_tensor if workspace_tensor is not None else workspace("pages", need, dev, stream)
+    # (with a single page there is no move, and its empty lists have no address)
+    none = _ptr(n_live)
+    _check(lib.tv_compact_pages(_ptr(block_table), _ptr(ref_count), B, mb, nb, base, size, count,
+                                none, _ptr(copy_src) or none, _ptr(copy_dst) or none, _ptr(ws),
+                                ws.numel(), stream))
+    return n_live, copy_src, copy_dst
 
 
 def block_causal_attention(q, k_ctx, v_ctx, k_blk, v_blk, anchors, out, scale=None,

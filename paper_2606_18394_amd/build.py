@@ -11,7 +11,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libtreeverify.so")
 SOURCES = ["tv_api.hip", "tv_attention.hip", "tv_accept.hip", "tv_draft.hip", "tv_cache.hip",
-           "tv_sample.hip", "tv_attention_fp8.hip"]
+           "tv_sample.hip", "tv_attention_fp8.hip", "tv_cache_fp8.hip", "tv_pages.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

@@ -11,9 +11,12 @@
 #include "treeverify.h"
 #include "tv_plan.h"
 #include "tv_plan_fp8.h"
+#include "tv_pages.h"
 
 static_assert(TV_MAX_NODES == tv::kMaxNodes, "node limit mismatch");
 static_assert(TV_MAX_DRAFT_DEPTH == tv::kMaxDraftDepth, "draft depth limit");
+static_assert(TV_MAX_POOLS == tv::kMaxPools && TV_MAX_FORKS == tv::kMaxForks &&
+              TV_MAX_RESERVE == tv::kMaxReserve, "page call limits");
 
 namespace tv {
 hipError_t launch_attention(const void* q, const void* kc, const void* vc, const void* kt,
@@ -35,6 +38,17 @@ hipError_t launch_commit(const void* kt, const void* vt, const int32_t* path,
                          const int32_t* accept_len, void* kc, void* vc, int32_t* kv_len,
                          const int32_t* block_table, int shift, int max_blocks, int num_blocks,
                          int B, int N, int Hkv, int D, int cap, int Dmax, hipStream_t st);
+hipError_t launch_write_fp8(const void* k, const void* v, const int32_t* n_new, const int32_t* path,
+                            void* k_pool, void* v_pool, uint8_t* k_exp, uint8_t* v_exp,
+                            const int32_t* block_table, int shift, int max_blocks, int num_blocks,
+                            int32_t* kv_len, int B, int T, int P, int Hkv, int D, hipStream_t st);
+hipError_t launch_reserve(const int32_t* n_rows, int32_t* table, const int32_t* kv_len, int32_t* ref,
+                          int32_t* ok, int B, int max_blocks, int shift, int num_blocks, hipStream_t st);
+hipError_t launch_fork(const ForkArgs& a, hipStream_t st);
+hipError_t launch_free(const int32_t* seqs, int n, int32_t* table, int32_t* kv_len, int32_t* ref, int B,
+                       int max_blocks, int num_blocks, hipStream_t st);
+hipError_t launch_copy(const CopyArgs& a, hipStream_t st);
+hipError_t launch_compact(const CompactArgs& a, hipStream_t st);
 hipError_t launch_accept(const void* logits, int f32, const int32_t* draft, const int32_t* parent,
                          int B, int N, int V, int Dmax, int32_t* accept_len, int32_t* path,
                          int32_t* tgt_out, void* ws, hipStream_t st);
@@ -335,6 +349,155 @@ int tv_commit_path_paged(const void* k_tree, const void* v_tree, const int32_t* 
                                    block_table, shift, max_blocks, num_blocks, B, N, Hkv, D,
                                    max_blocks * block_size, Dmax, stream);
   return e == hipSuccess ? TV_OK : TV_ERR_LAUNCH;
+}
+
+// Appending P rows at most of x [B, T, Hkv, D] to the 8-bit cache.
+static int check_write_fp8(const void* k, const void* v, const void* k_pool, const void* v_pool,
+                           const uint8_t* k_exp, const uint8_t* v_exp, const int32_t* block_table,
+                           int block_size, int max_blocks, int num_blocks, const int32_t* kv_len, int B,
+                           int T, int P, int Hkv, int D) {
+  const int rc = check_pages_fp8(Hkv, block_size, max_blocks, num_blocks);
+  if (rc != TV_OK) return rc;
+  if (B < 1 || T < 1 || P < 1 || max_blocks < 1 || num_blocks < 1) return TV_ERR_SHAPE;
+  if (D != 64 && D != 128) return TV_ERR_UNSUPPORTED;
+  // (a wave per group, head, and K or V)
+  if ((long long)B * Hkv > (1ll << 31) / ((P + 30ll) / 32 + 1)) return TV_ERR_UNSUPPORTED;
+  if (!k || !v || !k_pool || !v_pool || !k_exp || !v_exp || !block_table || !kv_len) return TV_ERR_NULL;
+  if (misaligned(k) || misaligned(v) || misaligned(k_pool) || misaligned(v_pool)) return TV_ERR_ALIGN;
+  return TV_OK;
+}
+
+int tv_append_paged_fp8(const void* k_new, const void* v_new, const int32_t* n_new, void* k_pool,
+                        void* v_pool, uint8_t* k_exp, uint8_t* v_exp, const int32_t* block_table,
+                        int block_size, int max_blocks, int num_blocks, int32_t* kv_len, int B, int T,
+                        int Hkv, int D, hipStream_t stream) {
+  const int rc = check_write_fp8(k_new, v_new, k_pool, v_pool, k_exp, v_exp, block_table, block_size,
+                                 max_blocks, num_blocks, kv_len, B, T, T, Hkv, D);
+  if (rc != TV_OK) return rc;
+  const hipError_t e = tv::launch_write_fp8(k_new, v_new, n_new, nullptr, k_pool, v_pool, k_exp, v_exp,
+                                            block_table, block_shift(block_size), max_blocks, num_blocks,
+                                            kv_len, B, T, T, Hkv, D, stream);
+  return e == hipSuccess ? TV_OK : TV_ERR_LAUNCH;
+}
+
+int tv_commit_path_paged_fp8(const void* k_tree, const void* v_tree, const int32_t* path,
+                             const int32_t* accept_len, void* k_pool, void* v_pool, uint8_t* k_exp,
+                             uint8_t* v_exp, const int32_t* block_table, int block_size, int max_blocks,
+                             int num_blocks, int32_t* kv_len, int B, int N, int Hkv, int D, int Dmax,
+                             hipStream_t stream) {
+  const int rc = check_write_fp8(k_tree, v_tree, k_pool, v_pool, k_exp, v_exp, block_table, block_size,
+                                 max_blocks, num_blocks, kv_len, B, N, Dmax, Hkv, D);
+  if (rc != TV_OK) return rc;
+  if (N > TV_MAX_NODES) return TV_ERR_UNSUPPORTED;
+  if (!path || !accept_len) return TV_ERR_NULL;
+  const hipError_t e = tv::launch_write_fp8(k_tree, v_tree, accept_len, path, k_pool, v_pool, k_exp,
+                                            v_exp, block_table, block_shift(block_size), max_blocks,
+                                            num_blocks, kv_len, B, N, Dmax, Hkv, D, stream);
+  return e == hipSuccess ? TV_OK : TV_ERR_LAUNCH;
+}
+
+// The page calls' common arguments; block_size 0 where the call has none.
+static int check_page_state(const int32_t* block_table, const int32_t* kv_len, const int32_t* ref_count,
+                            int B, int max_blocks, int block_size, int num_blocks) {
+  if (B < 1 || max_blocks < 1 || num_blocks < 1) return TV_ERR_SHAPE;
+  if (block_size != 0) {
+    if (block_shift(block_size) < 0) return TV_ERR_SHAPE;
+    if ((long long)max_blocks * block_size > (1ll << 30)) return TV_ERR_UNSUPPORTED;
+  }
+  if (num_blocks > (1 << 30) || (long long)B * max_blocks > (1ll << 31)) return TV_ERR_UNSUPPORTED;
+  return block_table && kv_len && ref_count ? TV_OK : TV_ERR_NULL;
+}
+
+static int fill_pools(void* const* pools, const int64_t* page_bytes, int n_pools, tv::Pools& p) {
+  p.n = n_pools;
+  p.total = 0;
+  if (n_pools < 0) return TV_ERR_SHAPE;
+  if (n_pools > TV_MAX_POOLS) return TV_ERR_UNSUPPORTED;
+  if (n_pools > 0 && (!pools || !page_bytes)) return TV_ERR_NULL;
+  for (int k = 0; k < n_pools; ++k) {
+    if (!pools[k]) return TV_ERR_NULL;
+    if (page_bytes[k] < 1) return TV_ERR_SHAPE;
+    if (page_bytes[k] > (1ll << 34)) return TV_ERR_UNSUPPORTED;
+    p.base[k] = pools[k];
+    p.page_bytes[k] = page_bytes[k];
+    p.pieces[k] = (int)((page_bytes[k] + tv::kPieceBytes - 1) / tv::kPieceBytes);
+    p.total += p.pieces[k];
+  }
+  return TV_OK;
+}
+
+int tv_reserve_pages(const int32_t* n_rows, int32_t* block_table, const int32_t* kv_len,
+                     int32_t* ref_count, int32_t* ok, int B, int max_blocks, int block_size,
+                     int num_blocks, hipStream_t stream) {
+  if (block_size < 1) return TV_ERR_SHAPE;
+  const int rc = check_page_state(block_table, kv_len, ref_count, B, max_blocks, block_size, num_blocks);
+  if (rc != TV_OK) return rc;
+  if (B > TV_MAX_RESERVE) return TV_ERR_UNSUPPORTED;
+  if (!n_rows || !ok) return TV_ERR_NULL;
+  const hipError_t e = tv::launch_reserve(n_rows, block_table, kv_len, ref_count, ok, B, max_blocks,
+                                          block_shift(block_size), num_blocks, stream);
+  return e == hipSuccess ? TV_OK : TV_ERR_LAUNCH;
+}
+
+int tv_fork_pages(const int32_t* src, const int32_t* dst, int n, int32_t* block_table, int32_t* kv_len,
+                  int32_t* ref_count, int B, int max_blocks, int block_size, int num_blocks,
+                  void* const* pools, const int64_t* page_bytes, int n_pools, int32_t* ok,
+                  int32_t* copy_src, int32_t* copy_dst, hipStream_t stream) {
+  if (block_size < 1 || n < 1) return TV_ERR_SHAPE;
+  int rc = check_page_state(block_table, kv_len, ref_count, B, max_blocks, block_size, num_blocks);
+  if (rc != TV_OK) return rc;
+  if (n > TV_MAX_FORKS) return TV_ERR_UNSUPPORTED;
+  if (!src || !dst || !ok || !copy_src || !copy_dst) return TV_ERR_NULL;
+  tv::ForkArgs a{src, dst, block_table, kv_len, ref_count, ok, copy_src, copy_dst, n, B, max_blocks,
+                 block_shift(block_size), num_blocks, {}};
+  if ((rc = fill_pools(pools, page_bytes, n_pools, a.pools)) != TV_OK) return rc;
+  return tv::launch_fork(a, stream) == hipSuccess ? TV_OK : TV_ERR_LAUNCH;
+}
+
+int tv_free_pages(const int32_t* seqs, int n, int32_t* block_table, int32_t* kv_len, int32_t* ref_count,
+                  int B, int max_blocks, int num_blocks, hipStream_t stream) {
+  if (n < 1) return TV_ERR_SHAPE;
+  const int rc = check_page_state(block_table, kv_len, ref_count, B, max_blocks, 0, num_blocks);
+  if (rc != TV_OK) return rc;
+  if (n > TV_MAX_RESERVE) return TV_ERR_UNSUPPORTED;
+  if (!seqs) return TV_ERR_NULL;
+  const hipError_t e = tv::launch_free(seqs, n, block_table, kv_len, ref_count, B, max_blocks,
+                                       num_blocks, stream);
+  return e == hipSuccess ? TV_OK : TV_ERR_LAUNCH;
+}
+
+int tv_copy_pages(const int32_t* src, const int32_t* dst, int n, int num_blocks, void* const* pools,
+                  const int64_t* page_bytes, int n_pools, hipStream_t stream) {
+  if (n < 1 || num_blocks < 1 || n_pools < 1) return TV_ERR_SHAPE;
+  if (num_blocks > (1 << 30)) return TV_ERR_UNSUPPORTED;
+  if (!src || !dst) return TV_ERR_NULL;
+  tv::CopyArgs a{src, dst, n, num_blocks, {}};
+  const int rc = fill_pools(pools, page_bytes, n_pools, a.pools);
+  if (rc != TV_OK) return rc;
+  return tv::launch_copy(a, stream) == hipSuccess ? TV_OK : TV_ERR_LAUNCH;
+}
+
+size_t tv_compact_pages_workspace(int num_blocks) {
+  if (num_blocks < 1 || num_blocks > (1 << 30)) return 0;
+  return ((size_t)num_blocks + tv::compact_runs(num_blocks) + 1) * 4;
+}
+
+int tv_compact_pages(int32_t* block_table, int32_t* ref_count, int B, int max_blocks, int num_blocks,
+                     void* const* pools, const int64_t* page_bytes, int n_pools, int32_t* n_live,
+                     int32_t* copy_src, int32_t* copy_dst, void* workspace, size_t workspace_bytes,
+                     hipStream_t stream) {
+  int rc = check_page_state(block_table, ref_count, ref_count, B, max_blocks, 0, num_blocks);
+  if (rc != TV_OK) return rc;
+  if (!n_live || !copy_src || !copy_dst) return TV_ERR_NULL;
+  tv::CompactArgs a{block_table, ref_count, n_live, copy_src, copy_dst, nullptr, nullptr, nullptr, B,
+                    max_blocks, num_blocks, {}};
+  if ((rc = fill_pools(pools, page_bytes, n_pools, a.pools)) != TV_OK) return rc;
+  if (!workspace || workspace_bytes < tv_compact_pages_workspace(num_blocks)) return TV_ERR_WORKSPACE;
+  if (misaligned(workspace)) return TV_ERR_ALIGN;
+  a.place = (int32_t*)workspace;
+  a.counts = a.place + num_blocks;
+  a.moves = a.counts + tv::compact_runs(num_blocks);
+  return tv::launch_compact(a, stream) == hipSuccess ? TV_OK : TV_ERR_LAUNCH;
 }
 
 size_t tv_tree_accept_workspace(int B, int N, int V) {

@@ -1,0 +1,400 @@
+// Whose page is whose, for CDNA4 (gfx950): pages of a paged cache are handed out, shared
+// between sequences, given back and drawn together, and their contents copied.
+//
+// State is what the caches use anyway plus a count: block_table [B, max_blocks] (a row's
+// pages come first, -1 behind them), kv_len [B] and ref_count [num_blocks], how many rows
+// name a page (0: free).  A new page is always the free one of the lowest number, so the
+// outcome depends on nothing but the arguments, and no list of free pages has to be kept:
+// finding them is one pass over ref_count, 4 bytes a page.  What many workgroups count at
+// once (pages shared or given back) are whole numbers, whose order of adding does not show.
+//
+// The deciding is latency, the copying HBM: a page is copied in pieces of 16 KB, a
+// workgroup each, of any pools whose first axis is the page.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "tv_pages.h"
+
+namespace tv {
+
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kDecide = 1024;  // threads of a deciding workgroup
+
+// Sum of x over the workgroup's threads before this one, and over all of them.
+__device__ __forceinline__ int block_scan(int x, int& total) {
+  __shared__ int sums[kDecide / 64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = (blockDim.x + 63) / 64;
+  int upto = x;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int y = __shfl_up(upto, d);
+    if (lane >= d) upto += y;
+  }
+  __syncthreads();  // the sums of a call before this one are read
+  if (lane == 63) sums[wave] = upto;
+  __syncthreads();
+  int before = 0;
+  total = 0;
+  for (int w = 0; w < waves; ++w) {
+    if (w == wave) before = total;
+    total += sums[w];
+  }
+  return before + upto - x;
+}
+
+// The free pages in increasing order, until `want` are found: emit(r, page) for the r-th.
+// Returns how many there are (at least `want`, or all).
+template <class Emit>
+__device__ __forceinline__ int find_free(const int32_t* ref, int num_blocks, int want, Emit emit) {
+  constexpr int kPer = 8;  // counts a thread reads in one go
+  int found = 0;
+  // (from a multiple of 16 bytes on, wherever ref begins)
+  for (long long at = -(long long)((uintptr_t)ref / 4 % 4); at < num_blocks && found < want;
+       at += kDecide * kPer) {
+    const long long first = at + (long long)threadIdx.x * kPer;
+    unsigned free = 0;
+    if (first >= 0 && first + kPer <= num_blocks) {
+      const int4 lo = *(const int4*)(ref + first), hi = *(const int4*)(ref + first + 4);
+      free = (lo.x <= 0) | (lo.y <= 0) << 1 | (lo.z <= 0) << 2 | (lo.w <= 0) << 3 | (hi.x <= 0) << 4 |
+             (hi.y <= 0) << 5 | (hi.z <= 0) << 6 | (hi.w <= 0) << 7;
+    } else {
+      for (int k = 0; k < kPer; ++k)
+        if (first + k >= 0 && first + k < num_blocks && ref[first + k] <= 0) free |= 1u << k;
+    }
+    int total;
+    int r = found + block_scan(__popc(free), total);
+    for (; free; free &= free - 1, ++r)
+      if (r < want) emit(r, (int)first + __ffs((int)free) - 1);
+    found += total;
+  }
+  return found;
+}
+
+// Pages for n_rows[b] more rows of every sequence.  One workgroup; a thread has
+// kSeqs consecutive sequences.
+struct ReserveArgs {
+  const int32_t* n_rows;
+  int32_t* table;
+  const int32_t* kv_len;
+  int32_t* ref;
+  int32_t* ok;
+  int B, max_blocks, shift, num_blocks;
+};
+constexpr int kSeqs = kMaxReserve / kDecide;
+
+__global__ __launch_bounds__(kDecide) void reserve_pages(ReserveArgs a) {
+  __shared__ int first_rank[kMaxReserve + 1], first_entry[kMaxReserve];
+  // what each sequence has, needs and is short of
+  int have[kSeqs], ask[kSeqs], mine = 0;
+  bool valid[kSeqs];
+#pragma unroll
+  for (int k = 0; k < kSeqs; ++k) {
+    const int b = threadIdx.x * kSeqs + k;
+    have[k] = ask[k] = 0;
+    valid[k] = false;
+    if (b >= a.B) continue;
+    const int kv = a.kv_len[b], n = a.n_rows[b], cap = a.max_blocks << a.shift;
+    valid[k] = kv >= 0 && n >= 0 && kv <= cap && n <= cap - kv;
+    if (!valid[k]) continue;
+    const int need = (kv + n + (1 << a.shift) - 1) >> a.shift;
+    // the first entry without a page, behind those of the rows that are there: a row's
+    // pages come first
+    const int32_t* row = a.table + (size_t)b * a.max_blocks;
+    int lo = (kv + (1 << a.shift) - 1) >> a.shift, hi = need;
+    for (int at = lo, step = 1; at < hi; at += step, step *= 2) {
+      if (row[at] < 0) hi = at;
+      else lo = at + 1;
+    }
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (row[mid] < 0) hi = mid;
+      else lo = mid + 1;
+    }
+    have[k] = lo;
+    ask[k] = need - lo;
+    mine += ask[k];
+  }
+  int total;
+  int rank = block_scan(mine, total);
+#pragma unroll
+  for (int k = 0; k < kSeqs; ++k) {
+    const int b = threadIdx.x * kSeqs + k;
+    first_rank[b] = rank;
+    first_entry[b] = have[k];
+    rank += ask[k];
+  }
+  if (threadIdx.x == 0) first_rank[kMaxReserve] = total;
+  __syncthreads();
+  // the r-th free page goes to the sequence whose ranks hold r
+  const int found = find_free(a.ref, a.num_blocks, total, [&](int r, int page) {
+    int lo = 0, hi = kMaxReserve;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (first_rank[mid] <= r) lo = mid;
+      else hi = mid;
+    }
+    a.table[(size_t)lo * a.max_blocks + first_entry[lo] + r - first_rank[lo]] = page;
+    a.ref[page] = 1;
+  });
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < kSeqs; ++k) {
+    const int b = threadIdx.x * kSeqs + k;
+    if (b >= a.B) continue;
+    const int r = first_rank[b];
+    const bool ok = valid[k] && (ask[k] == 0 || r + ask[k] <= found);
+    a.ok[b] = ok;
+    if (!ok && valid[k])  // short of pages: the ones it got go back
+      for (int j = 0; j < found - r && j < ask[k]; ++j) {
+        int32_t* entry = a.table + (size_t)b * a.max_blocks + have[k] + j;
+        a.ref[*entry] = 0;
+        *entry = -1;
+      }
+  }
+}
+
+// Forks, first half: which are possible, and which page each one's partly filled page is
+// copied to.  One workgroup, a thread per fork.
+__global__ __launch_bounds__(kDecide) void fork_decide(ForkArgs a) {
+  __shared__ int to[kDecide], fresh[kDecide];
+  const int i = threadIdx.x;
+  const int src = i < a.n ? a.src[i] : -1, dst = i < a.n ? a.dst[i] : -1;
+  to[i] = dst;
+  __syncthreads();
+  bool ok = src >= 0 && src < a.B && dst >= 0 && dst < a.B;
+  int kv = 0;
+  if (ok) {
+    kv = a.kv_len[src];
+    ok = kv >= 0 && kv <= (a.max_blocks << a.shift) && a.table[(size_t)dst * a.max_blocks] < 0;
+  }
+  for (int j = 0; j < a.n; ++j) ok = ok && to[j] != src && (j >= i || to[j] != dst);
+  const bool part = ok && (kv & ((1 << a.shift) - 1)) != 0;
+  int total;
+  const int rank = block_scan(part, total);
+  const int found = find_free(a.ref, a.num_blocks, total, [&](int r, int page) { fresh[r] = page; });
+  __syncthreads();
+  if (i >= a.n) return;
+  const bool copies = part && rank < found;
+  ok = ok && (!part || copies);
+  a.ok[i] = ok;
+  int from = -1;
+  if (copies) from = a.table[(size_t)src * a.max_blocks + (kv >> a.shift)];
+  a.copy_src[i] = from;
+  a.copy_dst[i] = copies ? fresh[rank] : -1;
+}
+
+// Moves piece `piece` of the pages from -> to, pools after each other, 16 KB a piece.
+__device__ __forceinline__ void copy_piece(const Pools& p, int from, int to, int piece) {
+  int k = 0;
+  while (piece >= p.pieces[k]) piece -= p.pieces[k++];
+  const long long bytes = p.page_bytes[k], at = (long long)piece * kPieceBytes;
+  const char* s = (const char*)p.base[k] + from * bytes + at;
+  char* d = (char*)p.base[k] + to * bytes + at;
+  const int len = (int)(bytes - at < kPieceBytes ? bytes - at : kPieceBytes);
+  if ((((uintptr_t)s | (uintptr_t)d | (uintptr_t)len) & 15) == 0) {
+    constexpr int kIn = kPieceBytes / 16 / kCopyThreads;
+    i32x4 v[kIn];
+#pragma unroll
+    for (int u = 0; u < kIn; ++u) {
+      const int c = (u * kCopyThreads + (int)threadIdx.x) * 16;
+      if (c < len) v[u] = *(const i32x4*)(s + c);
+    }
+#pragma unroll
+    for (int u = 0; u < kIn; ++u) {
+      const int c = (u * kCopyThreads + (int)threadIdx.x) * 16;
+      if (c < len) *(i32x4*)(d + c) = v[u];
+    }
+  } else {
+    for (int c = threadIdx.x; c < len; c += kCopyThreads) d[c] = s[c];
+  }
+}
+
+// Second half: shared pages, the child's row and length, and the copies.  A row of
+// workgroups per fork; the first does the bookkeeping.
+__global__ __launch_bounds__(kCopyThreads) void fork_do(ForkArgs a) {
+  const int i = blockIdx.x;
+  if (!a.ok[i]) return;
+  const int src = a.src[i], dst = a.dst[i], from = a.copy_src[i], to = a.copy_dst[i];
+  if (blockIdx.y == 0) {
+    const int kv = a.kv_len[src], full = kv >> a.shift;
+    const int32_t* row = a.table + (size_t)src * a.max_blocks;
+    int32_t* mine = a.table + (size_t)dst * a.max_blocks;
+    for (int j = threadIdx.x; j < a.max_blocks; j += kCopyThreads) {
+      int page = -1;
+      if (j < full) {
+        page = row[j];
+        if (page >= 0 && page < a.num_blocks) atomicAdd(a.ref + page, 1);
+      } else if (j == full && to >= 0) {
+        page = to;
+        a.ref[page] = 1;
+      }
+      mine[j] = page;
+    }
+    if (threadIdx.x == 0) a.kv_len[dst] = kv;
+  }
+  if (from < 0 || from >= a.num_blocks || to < 0) return;
+  for (int piece = blockIdx.y; piece < a.pools.total; piece += gridDim.y)
+    copy_piece(a.pools, from, to, piece);
+}
+
+__global__ __launch_bounds__(256) void free_pages(const int32_t* seqs, int n, int32_t* table,
+                                                  int32_t* kv_len, int32_t* ref, int B, int max_blocks,
+                                                  int num_blocks) {
+  const int i = blockIdx.x, b = seqs[i];
+  bool skip = b < 0 || b >= B;
+  for (int j = threadIdx.x; j < i; j += 256) skip |= seqs[j] == b;  // named before
+  if (__syncthreads_or(skip)) return;
+  int32_t* row = table + (size_t)b * max_blocks;
+  for (int j = threadIdx.x; j < max_blocks; j += 256) {
+    const int page = row[j];
+    if (page < 0) continue;
+    if (page < num_blocks && atomicSub(ref + page, 1) <= 0) atomicAdd(ref + page, 1);
+    row[j] = -1;
+  }
+  if (threadIdx.x == 0) kv_len[b] = 0;
+}
+
+__global__ __launch_bounds__(kCopyThreads) void copy_pages(CopyArgs a) {
+  const long long items = (long long)a.n * a.pools.total;
+  for (long long w = blockIdx.x; w < items; w += gridDim.x) {
+    const int i = (int)(w / a.pools.total);
+    const int from = a.src[i], to = a.dst[i];
+    if (from < 0 || to < 0 || from >= a.num_blocks || to >= a.num_blocks || from == to) continue;
+    copy_piece(a.pools, from, to, (int)(w % a.pools.total));
+  }
+}
+
+// Compaction.  With L live pages, free pages below L and live ones from L on are equally
+// many; the d-th such free page (upwards) takes the d-th such live one (downwards).  With
+// P(x) live pages below x: free x < L has d = x - P(x), live x >= L has d = L - 1 - P(x).
+// Three kernels: counts per run of pages; places; then copies, counts and tables.
+__device__ __forceinline__ unsigned live_of(const CompactArgs& a, long long first, int& n) {
+  unsigned live = 0;
+  n = 0;
+#pragma unroll
+  for (int k = 0; k < kCompactPer; ++k)
+    if (first + k < a.num_blocks && a.ref[first + k] > 0) live |= 1u << k;
+  n = __popc(live);
+  return live;
+}
+
+__global__ __launch_bounds__(kDecide) void compact_count(CompactArgs a) {
+  const long long first = ((long long)blockIdx.x * kDecide + threadIdx.x) * kCompactPer;
+  int n, total;
+  live_of(a, first, n);
+  block_scan(n, total);
+  if (threadIdx.x == 0) a.counts[blockIdx.x] = total;
+  for (int k = 0; k < kCompactPer; ++k) {
+    const long long x = first + k;
+    if (x < a.num_blocks) a.place[x] = -1;
+    if (x < a.num_blocks / 2) a.copy_src[x] = a.copy_dst[x] = -1;
+  }
+}
+
+__global__ __launch_bounds__(kDecide) void compact_place(CompactArgs a) {
+  const int runs = gridDim.x;
+  int before = 0, all = 0, sum;
+  for (int r = threadIdx.x; r < runs; r += kDecide) {
+    const int c = a.counts[r];
+    all += c;
+    before += r < (int)blockIdx.x ? c : 0;
+  }
+  block_scan(before, sum);
+  before = sum;
+  block_scan(all, sum);
+  const int L = sum;
+  const long long first = ((long long)blockIdx.x * kDecide + threadIdx.x) * kCompactPer;
+  int n, total;
+  const unsigned live = live_of(a, first, n);
+  int P = before + block_scan(n, total);
+  for (int k = 0; k < kCompactPer; ++k) {
+    const long long x = first + k;
+    if (x >= a.num_blocks) break;
+    const bool is = live >> k & 1;
+    if (x == L) *a.moves = L - P;
+    if (!is && x < L) a.copy_dst[x - P] = (int)x;
+    if (is && x >= L) {
+      a.copy_src[L - 1 - P] = (int)x;
+      a.place[x] = L - 1 - P;
+    }
+    P += is;
+  }
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    *a.n_live = L;
+    if (L >= a.num_blocks) *a.moves = 0;
+  }
+}
+
+__global__ __launch_bounds__(kCopyThreads) void compact_move(CompactArgs a) {
+  const int moves = *a.moves;
+  if (moves == 0) return;
+  const long long me = (long long)blockIdx.x * kCopyThreads + threadIdx.x;
+  const long long all = (long long)gridDim.x * kCopyThreads;
+  for (long long t = me; t < (long long)a.B * a.max_blocks; t += all) {
+    const int page = a.table[t];
+    if (page < 0 || page >= a.num_blocks) continue;
+    const int d = a.place[page];
+    if (d >= 0) a.table[t] = a.copy_dst[d];
+  }
+  for (long long d = me; d < moves; d += all) {
+    const int from = a.copy_src[d];
+    a.ref[a.copy_dst[d]] = a.ref[from];
+    a.ref[from] = 0;
+  }
+  const long long items = (long long)moves * a.pools.total;
+  for (long long w = blockIdx.x; w < items; w += gridDim.x) {
+    const int d = (int)(w / a.pools.total);
+    copy_piece(a.pools, a.copy_src[d], a.copy_dst[d], (int)(w % a.pools.total));
+  }
+}
+
+// ------------------------------------------------------------------ launches
+
+static unsigned copy_grid(long long items) { return (unsigned)(items < 4096 ? items : 4096); }
+
+hipError_t launch_reserve(const int32_t* n_rows, int32_t* table, const int32_t* kv_len, int32_t* ref,
+                          int32_t* ok, int B, int max_blocks, int shift, int num_blocks, hipStream_t st) {
+  hipLaunchKernelGGL(reserve_pages, dim3(1), dim3(kDecide), 0, st,
+                     (ReserveArgs{n_rows, table, kv_len, ref, ok, B, max_blocks, shift, num_blocks}));
+  return hipGetLastError();
+}
+
+hipError_t launch_fork(const ForkArgs& a, hipStream_t st) {
+  hipLaunchKernelGGL(fork_decide, dim3(1), dim3(kDecide), 0, st, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const int pieces = a.pools.total < 1 ? 1 : (a.pools.total < 64 ? a.pools.total : 64);
+  hipLaunchKernelGGL(fork_do, dim3(a.n, pieces), dim3(kCopyThreads), 0, st, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_free(const int32_t* seqs, int n, int32_t* table, int32_t* kv_len, int32_t* ref, int B,
+                       int max_blocks, int num_blocks, hipStream_t st) {
+  hipLaunchKernelGGL(free_pages, dim3(n), dim3(256), 0, st, seqs, n, table, kv_len, ref, B, max_blocks,
+                     num_blocks);
+  return hipGetLastError();
+}
+
+hipError_t launch_copy(const CopyArgs& a, hipStream_t st) {
+  const long long items = (long long)a.n * a.pools.total;
+  if (items == 0) return hipSuccess;
+  hipLaunchKernelGGL(copy_pages, dim3(copy_grid(items)), dim3(kCopyThreads), 0, st, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_compact(const CompactArgs& a, hipStream_t st) {
+  const dim3 runs((unsigned)compact_runs(a.num_blocks));
+  hipLaunchKernelGGL(compact_count, runs, dim3(kDecide), 0, st, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(compact_place, runs, dim3(kDecide), 0, st, a);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  const long long items = (long long)(a.num_blocks / 2) * a.pools.total;
+  const long long rows = ((long long)a.B * a.max_blocks + kCopyThreads - 1) / kCopyThreads;
+  const long long most = items > rows ? items : rows;
+  hipLaunchKernelGGL(compact_move, dim3(copy_grid(most < 1 ? 1 : most)), dim3(kCopyThreads), 0, st, a);
+  return hipGetLastError();
+}
+
+}  // namespace tv

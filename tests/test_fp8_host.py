@@ -62,3 +62,117 @@ def test_binding_refuses_host_tensors_and_types():
         binding.tree_verify_attention_paged_fp8(**t)
     with pytest.raises(TypeError, match="q must be"):
         binding.tree_verify_attention_paged_fp8(**{**t, "q": t["q"].float()})
+
+
+def _append(**kw):
+    a = dict(k=FAKE, v=FAKE, n=None, kp=FAKE, vp=FAKE, ke=FAKE + 1, ve=FAKE + 3, bt=FAKE, bs=64, mb=64,
+             nb=500, kv=FAKE, B=4, T=16, Hkv=8, D=128)
+    assert not set(kw) - set(a)
+    a.update(kw)
+    return _lib().tv_append_paged_fp8(
+        a["k"], a["v"], a["n"], a["kp"], a["vp"], a["ke"], a["ve"], a["bt"], a["bs"], a["mb"], a["nb"],
+        a["kv"], a["B"], a["T"], a["Hkv"], a["D"], None)
+
+
+def _commit(**kw):
+    a = dict(k=FAKE, v=FAKE, path=FAKE, n=FAKE, kp=FAKE, vp=FAKE, ke=FAKE + 1, ve=FAKE + 3, bt=FAKE, bs=64,
+             mb=64, nb=500, kv=FAKE, B=4, N=16, Hkv=8, D=128, Dmax=5)
+    assert not set(kw) - set(a)
+    a.update(kw)
+    return _lib().tv_commit_path_paged_fp8(
+        a["k"], a["v"], a["path"], a["n"], a["kp"], a["vp"], a["ke"], a["ve"], a["bt"], a["bs"], a["mb"],
+        a["nb"], a["kv"], a["B"], a["N"], a["Hkv"], a["D"], a["Dmax"], None)
+
+
+WRITE = [
+    (NULL, dict(k=None)), (NULL, dict(v=None)), (NULL, dict(kp=None)), (NULL, dict(vp=None)),
+    (NULL, dict(ke=None)), (NULL, dict(ve=None)), (NULL, dict(bt=None)), (NULL, dict(kv=None)),
+    (SHAPE, dict(B=0)), (SHAPE, dict(Hkv=0)), (SHAPE, dict(mb=0)), (SHAPE, dict(nb=0)), (SHAPE, dict(bs=33)),
+    (SHAPE, dict(bs=16)), (UNSUPPORTED, dict(D=32)), (UNSUPPORTED, dict(mb=1 << 30)),
+    (UNSUPPORTED, dict(nb=1 << 30)), (UNSUPPORTED, dict(B=(1 << 31) - 1)),
+    (ALIGN, dict(k=FAKE + 8)), (ALIGN, dict(v=FAKE + 2)), (ALIGN, dict(kp=FAKE + 8)),
+    (ALIGN, dict(vp=FAKE + 8)),
+]
+
+
+@pytest.mark.parametrize("code, bad", WRITE + [(SHAPE, dict(T=0))])
+def test_append_refuses(code, bad):
+    assert _append(**bad) == code
+
+
+@pytest.mark.parametrize("code, bad", WRITE + [(SHAPE, dict(N=0)), (SHAPE, dict(Dmax=0)),
+                                               (UNSUPPORTED, dict(N=2049)), (NULL, dict(path=None)),
+                                               (NULL, dict(n=None))])
+def test_commit_refuses(code, bad):
+    assert _commit(**bad) == code
+
+
+def _pools(n, size=64, base=FAKE):
+    return (ctypes.c_void_p * n)(*[base] * n), (ctypes.c_int64 * n)(*[size] * n), n
+
+
+def test_page_calls_refuse():
+    lib = _lib()
+
+    def reserve(n=FAKE, bt=FAKE, kv=FAKE, ref=FAKE, ok=FAKE, B=4, mb=8, bs=64, nb=100):
+        return lib.tv_reserve_pages(n, bt, kv, ref, ok, B, mb, bs, nb, None)
+
+    def fork(src=FAKE, dst=FAKE, n=3, bt=FAKE, kv=FAKE, ref=FAKE, B=4, mb=8, bs=64, nb=100, pools=_pools(2),
+             ok=FAKE, cs=FAKE, cd=FAKE):
+        return lib.tv_fork_pages(src, dst, n, bt, kv, ref, B, mb, bs, nb, *pools, ok, cs, cd, None)
+
+    def free(seqs=FAKE, n=3, bt=FAKE, kv=FAKE, ref=FAKE, B=4, mb=8, nb=100):
+        return lib.tv_free_pages(seqs, n, bt, kv, ref, B, mb, nb, None)
+
+    def copy(src=FAKE, dst=FAKE, n=3, nb=100, pools=_pools(2)):
+        return lib.tv_copy_pages(src, dst, n, nb, *pools, None)
+
+    def compact(bt=FAKE, ref=FAKE, B=4, mb=8, nb=100, pools=_pools(2), live=FAKE, cs=FAKE, cd=FAKE, ws=FAKE,
+                wsb=1 << 20):
+        return lib.tv_compact_pages(bt, ref, B, mb, nb, *pools, live, cs, cd, ws, wsb, None)
+
+    for call in (reserve, fork, free):
+        assert call(bt=None) == call(kv=None) == call(ref=None) == NULL
+        assert call(B=0) == call(mb=0) == call(nb=0) == SHAPE
+        assert call(nb=(1 << 30) + 1) == call(B=1 << 20, mb=1 << 20) == UNSUPPORTED
+    for call in (reserve, fork):
+        assert call(bs=0) == call(bs=-64) == call(bs=48) == call(bs=16) == SHAPE
+        assert call(mb=1 << 28) == UNSUPPORTED and call(ok=None) == NULL
+    assert reserve(n=None) == NULL and reserve(B=4097) == UNSUPPORTED
+    for call in (fork, copy):
+        assert call(src=None) == call(dst=None) == NULL and call(n=0) == SHAPE
+    assert fork(n=1025) == UNSUPPORTED and fork(cs=None) == fork(cd=None) == NULL
+    assert free(seqs=None) == NULL and free(n=0) == SHAPE and free(n=4097) == UNSUPPORTED
+    for call in (fork, copy, compact):
+        assert call(pools=_pools(65)) == UNSUPPORTED and call(pools=(None, None, 2)) == NULL
+        assert call(pools=_pools(2, base=None)) == NULL and call(pools=_pools(2, size=0)) == SHAPE
+        assert call(pools=(*_pools(2)[:2], -1)) == SHAPE
+        assert call(pools=_pools(2, size=1 << 35)) == UNSUPPORTED
+    assert copy(nb=0) == copy(pools=_pools(0)) == SHAPE
+    assert compact(bt=None) == compact(ref=None) == compact(live=None) == compact(cs=None) == NULL
+    assert compact(ws=None) == compact(wsb=400) == WORKSPACE and compact(ws=FAKE + 8) == ALIGN
+    need = lib.tv_compact_pages_workspace
+    assert need(1) >= 4 and need(0) == need(-5) == need((1 << 30) + 1) == 0
+
+
+def test_binding_checks_pages():
+    i32 = torch.int32
+    bt, kv, ref = torch.zeros(2, 3, dtype=i32), torch.zeros(2, dtype=i32), torch.zeros(5, dtype=i32)
+    for call in (lambda: binding.reserve_pages(kv, bt, kv, ref, 64),
+                 lambda: binding.fork_pages(kv, kv, bt, kv, ref, 64),
+                 lambda: binding.free_pages(kv, bt, kv, ref),
+                 lambda: binding.copy_pages(kv, kv, [torch.zeros(5, 4)]),
+                 lambda: binding.compact_pages(bt, ref)):
+        with pytest.raises(ValueError, match="GPU tensor"):
+            call()
+    with pytest.raises(ValueError, match="at least one pool"):
+        binding.copy_pages(kv, kv, [])
+    with pytest.raises(ValueError, match="expected 5 pages"):
+        binding._pool_arrays([torch.zeros(4, 2)], 5, torch.device("cpu"))
+    t = _tensors()
+    with pytest.raises(ValueError, match="GPU tensor"):
+        binding.append_paged_fp8(t["k_tree"], t["v_tree"], t["k_pool"], t["v_pool"], t["k_exp"],
+                                 t["v_exp"], bt, kv)
+    with pytest.raises(ValueError, match="GPU tensor"):
+        binding.commit_path_paged_fp8(t["k_tree"], t["v_tree"], bt, kv, t["k_pool"], t["v_pool"],
+                                      t["k_exp"], t["v_exp"], bt, kv)
