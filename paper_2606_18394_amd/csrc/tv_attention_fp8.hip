@@ -99,24 +99,44 @@ __device__ __forceinline__ void interleave() {
   }
 }
 
+// A tile's codes in a wave's registers, as the products take them.
+template <int D>
+struct Codes {
+  i32x4 k[2][D / 64];
+  i32x2 v[D / 16];
+};
+// (The tile begins at a multiple of 128 bytes.)
+template <int D>
+__device__ __forceinline__ void read_keys(uint32_t lds, Codes<D>& t, int g4, int l16) {
+  using CL = CodeLayout<D>;
+  const uint32_t k0 = lds + CL::off(l16, g4);
+#pragma unroll
+  for (int p = 0; p < D / 64; ++p)
+#pragma unroll
+    for (int tt = 0; tt < 2; ++tt)
+      t.k[tt][p] = *((lds_i32x4*)(k0 ^ (64 * p) ^ (CL::kFlip * tt)) + tt * D);
+}
+template <int D>
+__device__ __forceinline__ void read_values(uint32_t lds, Codes<D>& t, int g4, int l16) {
+  using CL = CodeLayout<D>;
+  const int r = l16 >> 1, row = 4 * g4 + r + (r < 4 ? 0 : 12);
+  const uint32_t v0 = lds + CL::off(row, 0) + 8 * (l16 & 1);
+#pragma unroll
+  for (int dt = 0; dt < D / 16; ++dt)
+    t.v[dt] = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2*)(v0 ^ (16 * dt)) + CL::kBytes / 8);
+}
+
 // One 32-key tile of codes for a wave's rows, with the scales of K and V.  The
 // conversions go between the products before theirs: a product keeps the matrix core
-// busy for 16 cycles and issues in 4.  The tile begins at a multiple of 128 bytes.
-template <int D, int NT, bool kMasked>
-__device__ __forceinline__ void attend_codes(uint32_t lds, float kscale, float vscale,
+// busy for 16 cycles and issues in 4.  The values are read behind the scores unless they
+// are there already (kHeld).
+template <int D, int NT, bool kMasked, bool kHeld>
+__device__ __forceinline__ void attend_codes(Codes<D>& t, uint32_t lds, float kscale, float vscale,
                                              const bf16x8 (&qf)[NT][D / 32], f32x4 (&o)[D / 16][NT],
                                              f32x4 (&lacc)[NT], float (&m)[NT], float (&thr)[NT],
                                              const bf16x8& ones, float c, float inv_c,
                                              const uint32_t (&bits)[NT], int g4, int l16) {
-  using CL = CodeLayout<D>;
   constexpr int NP = D / 64, DT = D / 16;
-  i32x4 kw[2][NP];
-  const uint32_t k0 = lds + CL::off(l16, g4);
-#pragma unroll
-  for (int p = 0; p < NP; ++p)
-#pragma unroll
-    for (int tt = 0; tt < 2; ++tt)
-      kw[tt][p] = *((lds_i32x4*)(k0 ^ (64 * p) ^ (CL::kFlip * tt)) + tt * D);
   pin_order();
   f32x4 sc[2][NT];
   __builtin_amdgcn_s_setprio(1);
@@ -127,8 +147,8 @@ __device__ __forceinline__ void attend_codes(uint32_t lds, float kscale, float v
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt) {
-        const i32x2 lo = from_codes(kw[tt][p][2 * h], kscale);
-        const i32x2 hi = from_codes(kw[tt][p][2 * h + 1], kscale);
+        const i32x2 lo = from_codes(t.k[tt][p][2 * h], kscale);
+        const i32x2 hi = from_codes(t.k[tt][p][2 * h + 1], kscale);
         kf[tt][2 * p + h] = __builtin_bit_cast(bf16x8, i32x4{lo[0], lo[1], hi[0], hi[1]});
       }
 #pragma unroll
@@ -145,12 +165,7 @@ __device__ __forceinline__ void attend_codes(uint32_t lds, float kscale, float v
   interleave<(2 * NP - 1) * 2 * NT, 1, 4 / NT>();
   pin_order();
   __builtin_amdgcn_s_setprio(0);
-  i32x2 vw[DT];
-  const int r = l16 >> 1, row = 4 * g4 + r + (r < 4 ? 0 : 12);
-  const uint32_t v0 = lds + CL::off(row, 0) + 8 * (l16 & 1);
-#pragma unroll
-  for (int dt = 0; dt < DT; ++dt)
-    vw[dt] = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2*)(v0 ^ (16 * dt)) + CL::kBytes / 8);
+  if (!kHeld) read_values<D>(lds, t, g4, l16);
   pin_order();
   if (kMasked) tile_mask<NT>(sc, bits, g4);
   tile_reference<DT, NT>(sc, m, thr, o, lacc, c, inv_c);
@@ -161,7 +176,7 @@ __device__ __forceinline__ void attend_codes(uint32_t lds, float kscale, float v
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-    for (int h = 0; h < 2; ++h) vf[dt][h] = __builtin_bit_cast(i16x4, from_codes(vw[dt][h], vscale));
+    for (int h = 0; h < 2; ++h) vf[dt][h] = __builtin_bit_cast(i16x4, from_codes(t.v[dt][h], vscale));
   tile_values<D, NT>(vf, pf, ones, o, lacc);
   interleave<DT, NT, 4>();
   pin_order();
@@ -191,21 +206,21 @@ __device__ __forceinline__ void attend_tree(const unsigned char* k_lds, const un
   tile_weights<NT>(sc, m, c, pf);
   pin_order();
   i16x4 vf[DT][2];
-  read_values<D>(v_lds, vf, g4, l16);
+  tv::read_values<D>(v_lds, vf, g4, l16);
   tile_values<D, NT>(vf, pf, ones, o, lacc);
 }
 
-// WR row groups x WK key groups of one wave64 each.  A wave owns 32 rows of its row
+// WR row groups x WK key groups of one wave64 each.  A wave owns 16 * NT rows of its row
 // group; the WR waves of a key group share a ring of NU units and walk that group's
 // tiles (every WK-th of the chunk) in lock step.
-template <int D, int WR, int WK, int NU>
+template <int D, int WR, int WK, int NT, int NU>
 __global__ __launch_bounds__(64 * WR * WK) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void attn_fp8(Fp8Args a) {
   using TL = TileLayout<D>;
   using CL = CodeLayout<D>;
   constexpr int kThreads = 64 * WR * WK, kWaves = WR * WK;
-  constexpr int RB = kRowsPerWave * WR;
-  constexpr int NT = kRowsPerWave / 16, NTG = RB / 16;
+  constexpr int kRows = 16 * NT, RB = kRows * WR, NTG = NT * WR;
+  constexpr bool kAlone = WR == 1;  // a wave with a ring of its own
   constexpr int NC = D / 32, DT = D / 16;
   constexpr int UNIT = 64 * D;
   constexpr int kDma = UNIT / 1024;                 // 1 KB DMA instructions per unit,
@@ -287,7 +302,7 @@ void attn_fp8(Fp8Args a) {
   }
 
   // ---- queries: B operand of S^T = K Q^T
-  const int wrow0 = r0 + kRowsPerWave * wr;
+  const int wrow0 = r0 + kRows * wr;
   bf16x8 qf[NT][NC];
   bool qok[NT];
 #pragma unroll
@@ -415,28 +430,27 @@ void attn_fp8(Fp8Args a) {
   const bool busy = wrow0 < a.M;  // else only the tiles are moved
   uint32_t bits[NT] = {};
   int head = 0;  // the next step's first unit
+  auto refill = [&]() {  // into what the steps before `head` took up
+    while (issued < n_units && issued < head + NU) {
+      if (issued < n_c && (issued & 63) == 0) {
+        group = group_of(issued);
+        loaded(group);
+      }
+      if (mover) issue_unit(issued);
+      ++issued;
+    }
+  };
   // Step i: its units are there once at most the later ones' DMAs are in flight; the
   // barrier makes the whole group's visible, and what the steps before took up is free.
   auto ring_step = [&](int i) {
     const bool mine = i < n_mine;
     const int next = head + (mine ? (i < n_c ? 1 : 2) : 0);
-    auto refill = [&]() {
-      while (issued < n_units && issued < head + NU) {
-        if (issued < n_c && (issued & 63) == 0) {
-          group = group_of(issued);
-          loaded(group);
-        }
-        if (mover) issue_unit(issued);
-        ++issued;
-      }
-    };
-    if (WR > 1) {
+    if (kAlone) {
+      if (mine) wait_tiles<PU, NU>(issued - next);
+    } else {
       if (mine && mover) wait_tiles<PU, NU>(issued - next);
       __syncthreads();
       if (i > 0) refill();
-    } else {
-      if (i > 0) refill();
-      if (mine) wait_tiles<PU, NU>(issued - next);
     }
     if (i > 0 && i < n_c && (i & 63) == 0) {
       const int at = group_of(i);
@@ -446,6 +460,16 @@ void attn_fp8(Fp8Args a) {
       loaded(vexp);
     }
     head = next;
+  };
+  // A wave alone frees a cache tile's place as soon as it holds the codes.
+  Codes<D> codes;
+  auto take = [&](uint32_t unit, int hg4, int hl16) {
+    read_keys<D>(unit, codes, hg4, hl16);
+    if (kAlone) {
+      read_values<D>(unit, codes, hg4, hl16);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      refill();
+    }
   };
   auto scale_of = [&](int exps, int i) {
     return __int_as_float(__builtin_amdgcn_readlane(exps, i & 63) << 23);
@@ -457,8 +481,9 @@ void attn_fp8(Fp8Args a) {
     const uint32_t unit = ring + (head % NU) * UNIT;
     ring_step(i);
     if (!busy) continue;
-    attend_codes<D, NT, false>(unit, scale_of(kexp, i), scale_of(vexp, i), qf, o, lacc, m, thr, ones,
-                               a.c, inv_c, bits, g4, l16);
+    take(unit, g4, l16);
+    attend_codes<D, NT, false, kAlone>(codes, unit, scale_of(kexp, i), scale_of(vexp, i), qf, o, lacc, m,
+                                       thr, ones, a.c, inv_c, bits, g4, l16);
   }
   for (; i < n_iter; ++i) {
     const int at = (head % NU) * UNIT, at_v = ((head + 1) % NU) * UNIT;
@@ -469,11 +494,14 @@ void attn_fp8(Fp8Args a) {
     int hg4 = g4, hl16 = l16;
     asm volatile("" : "+v"(hg4), "+v"(hl16));
     tile_bits<NT>(MaskInfo{t0 + wk + WK * i, nct, kvl, ntt, 0, anc}, node_rel, bits);
-    if (i < n_c)
-      attend_codes<D, NT, true>(ring + at, scale_of(kexp, i), scale_of(vexp, i), qf, o, lacc, m, thr, ones,
-                                a.c, inv_c, bits, hg4, hl16);
-    else
+    if (i < n_c) {
+      take(ring + at, hg4, hl16);
+      attend_codes<D, NT, true, kAlone>(codes, ring + at, scale_of(kexp, i), scale_of(vexp, i), qf, o, lacc,
+                                        m, thr, ones, a.c, inv_c, bits, hg4, hl16);
+    } else {
       attend_tree<D, NT>(ring_ptr + at, ring_ptr + at_v, qf, o, lacc, m, thr, ones, a.c, inv_c, bits, hg4, hl16);
+      if (kAlone) refill();
+    }
   }
 
   const LateArgs* z = late_args();
@@ -518,7 +546,7 @@ void attn_fp8(Fp8Args a) {
     // ---- merge the WK key groups of each row group (same rows, disjoint keys)
     __syncthreads();  // rings and tree tables are dead from here on
     f32x4* obuf = reinterpret_cast<f32x4*>(smem);
-    float2* mlbuf = reinterpret_cast<float2*>(smem + (size_t)kWaves * kRowsPerWave * D * 4);
+    float2* mlbuf = reinterpret_cast<float2*>(smem + (size_t)kWaves * kRows * D * 4);
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
@@ -526,7 +554,7 @@ void attn_fp8(Fp8Args a) {
     if (g4 == 0) {
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
-        mlbuf[wave * kRowsPerWave + nt * 16 + l16] = make_float2(m[nt], lsum[nt]);
+        mlbuf[wave * kRows + nt * 16 + l16] = make_float2(m[nt], lsum[nt]);
     }
     __syncthreads();
     for (int f = wk; f < DT * NT; f += WK) {
@@ -536,7 +564,7 @@ void attn_fp8(Fp8Args a) {
       float mw[WK], mstar = -INFINITY;
 #pragma unroll
       for (int k = 0; k < WK; ++k) {
-        mw[k] = mlbuf[(k * WR + wr) * kRowsPerWave + rw].x;
+        mw[k] = mlbuf[(k * WR + wr) * kRows + rw].x;
         mstar = fmaxf(mstar, mw[k]);
       }
       f32x4 acc = {0.f, 0.f, 0.f, 0.f};
@@ -544,7 +572,7 @@ void attn_fp8(Fp8Args a) {
 #pragma unroll
       for (int k = 0; k < WK; ++k) {
         const float e = mw[k] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mw[k] - mstar);
-        l += e * mlbuf[(k * WR + wr) * kRowsPerWave + rw].y;
+        l += e * mlbuf[(k * WR + wr) * kRows + rw].y;
         acc += e * obuf[(((k * WR + wr) * DT + dt) * NT + nt) * 64 + lane];
       }
       emit(dt, wr * NT + nt, acc, mstar, l);
@@ -568,15 +596,16 @@ void attn_fp8(Fp8Args a) {
   __syncthreads();
   if (!s_last) return;
   const bool bad = __hip_atomic_load(z->tree_bad + grp, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != 0;
-  merge_chunks<D, RB, kWaves>(z, part0, nval, b, g, r0, bad, wave, lane);
+  constexpr int kMerge = kWaves < NTG * DT ? kWaves : NTG * DT;  // a wave per fragment at most
+  if (wave < kMerge) merge_chunks<D, RB, kMerge>(z, part0, nval, b, g, r0, bad, wave, lane);
 }
 
 hipError_t launch_combine(const AttnArgs& a, int D, int RB, hipStream_t st);  // tv_attention.hip
 
 template <int D, int ARR>
 static hipError_t launch_fp8_t(const Fp8Args& a, const AttnPlan& p, hipStream_t st) {
-  constexpr Arrangement ar = kArrangementsFp8[ARR];
-  constexpr auto kernel = &attn_fp8<D, ar.WR, ar.WK, arr_stages(ar, D)>;
+  constexpr ArrangementFp8 ar = kArrangementsFp8[ARR];
+  constexpr auto kernel = &attn_fp8<D, ar.WR, ar.WK, ar.NT, D == 128 ? ar.NU128 : ar.NU64>;
   // the kernel's LDS limit on each device, raised only when a call needs more
   constexpr int kDevices = 64;
   static std::atomic<int> limit[kDevices];

@@ -43,29 +43,46 @@ __device__ __forceinline__ int block_scan(int x, int& total) {
   return before + upto - x;
 }
 
-// The free pages in increasing order, until `want` are found: emit(r, page) for the r-th.
+// Which of a thread's kRun pages from `first` on are free, as a bit mask.
+constexpr int kRun = 8;
+__device__ __forceinline__ unsigned free_mask(const int32_t* ref, int num_blocks, long long first) {
+  unsigned free = 0;
+  if (first >= 0 && first + kRun <= num_blocks) {
+    const int4 lo = *(const int4*)(ref + first), hi = *(const int4*)(ref + first + 4);
+    free = (lo.x <= 0) | (lo.y <= 0) << 1 | (lo.z <= 0) << 2 | (lo.w <= 0) << 3 | (hi.x <= 0) << 4 |
+           (hi.y <= 0) << 5 | (hi.z <= 0) << 6 | (hi.w <= 0) << 7;
+  } else {
+    for (int k = 0; k < kRun; ++k)
+      if (first + k >= 0 && first + k < num_blocks && ref[first + k] <= 0) free |= 1u << k;
+  }
+  return free;
+}
+
+// The first page of the workgroup's first pass over ref_count, whose runs begin at
+// multiples of 16 bytes wherever it begins; a pass takes kDecide * kRun pages.
+__device__ __forceinline__ long long pass_start(const int32_t* ref) {
+  return -(long long)((uintptr_t)ref / 4 % 4);
+}
+
+// The free pages in increasing order, until `want` are found.  Those of a pass, at most
+// kDecide * kRun, go to `list`, counted from page `base` on; use(r0, n, base) then has the
+// r0-th to the (r0 + n - 1)-th there.
+// `ahead`: free_mask of the thread's first run, asked for before the caller knew `want`.
 // Returns how many there are (at least `want`, or all).
-template <class Emit>
-__device__ __forceinline__ int find_free(const int32_t* ref, int num_blocks, int want, Emit emit) {
-  constexpr int kPer = 8;  // counts a thread reads in one go
+template <class Use>
+__device__ __forceinline__ int find_free(const int32_t* ref, int num_blocks, int want, unsigned ahead,
+                                         uint16_t* list, Use use) {
   int found = 0;
-  // (from a multiple of 16 bytes on, wherever ref begins)
-  for (long long at = -(long long)((uintptr_t)ref / 4 % 4); at < num_blocks && found < want;
-       at += kDecide * kPer) {
-    const long long first = at + (long long)threadIdx.x * kPer;
-    unsigned free = 0;
-    if (first >= 0 && first + kPer <= num_blocks) {
-      const int4 lo = *(const int4*)(ref + first), hi = *(const int4*)(ref + first + 4);
-      free = (lo.x <= 0) | (lo.y <= 0) << 1 | (lo.z <= 0) << 2 | (lo.w <= 0) << 3 | (hi.x <= 0) << 4 |
-             (hi.y <= 0) << 5 | (hi.z <= 0) << 6 | (hi.w <= 0) << 7;
-    } else {
-      for (int k = 0; k < kPer; ++k)
-        if (first + k >= 0 && first + k < num_blocks && ref[first + k] <= 0) free |= 1u << k;
-    }
+  for (long long at = pass_start(ref); at < num_blocks && found < want; at += kDecide * kRun) {
+    const long long first = at + (long long)threadIdx.x * kRun;
+    unsigned free = at <= 0 ? ahead : free_mask(ref, num_blocks, first);
     int total;
-    int r = found + block_scan(__popc(free), total);
-    for (; free; free &= free - 1, ++r)
-      if (r < want) emit(r, (int)first + __ffs((int)free) - 1);
+    int r = block_scan(__popc(free), total);
+    const int most = min(total, want - found);
+    for (; free && r < most; free &= free - 1) list[r++] = (uint16_t)(threadIdx.x * kRun + __ffs((int)free) - 1);
+    __syncthreads();
+    use(found, most, (int)at);
+    __syncthreads();
     found += total;
   }
   return found;
@@ -85,6 +102,9 @@ constexpr int kSeqs = kMaxReserve / kDecide;
 
 __global__ __launch_bounds__(kDecide) void reserve_pages(ReserveArgs a) {
   __shared__ int first_rank[kMaxReserve + 1], first_entry[kMaxReserve];
+  __shared__ uint16_t list[kDecide * kRun];
+  const unsigned ahead =
+      free_mask(a.ref, a.num_blocks, pass_start(a.ref) + (long long)threadIdx.x * kRun);
   // what each sequence has, needs and is short of
   int have[kSeqs], ask[kSeqs], mine = 0;
   bool valid[kSeqs];
@@ -127,15 +147,18 @@ __global__ __launch_bounds__(kDecide) void reserve_pages(ReserveArgs a) {
   if (threadIdx.x == 0) first_rank[kMaxReserve] = total;
   __syncthreads();
   // the r-th free page goes to the sequence whose ranks hold r
-  const int found = find_free(a.ref, a.num_blocks, total, [&](int r, int page) {
-    int lo = 0, hi = kMaxReserve;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (first_rank[mid] <= r) lo = mid;
-      else hi = mid;
+  const int found = find_free(a.ref, a.num_blocks, total, ahead, list, [&](int r0, int n, int base) {
+    for (int i = threadIdx.x; i < n; i += kDecide) {
+      const int r = r0 + i, page = base + list[i];
+      int lo = 0, hi = a.B;
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (first_rank[mid] <= r) lo = mid;
+        else hi = mid;
+      }
+      a.table[(size_t)lo * a.max_blocks + first_entry[lo] + r - first_rank[lo]] = page;
+      a.ref[page] = 1;
     }
-    a.table[(size_t)lo * a.max_blocks + first_entry[lo] + r - first_rank[lo]] = page;
-    a.ref[page] = 1;
   });
   __syncthreads();
 #pragma unroll
@@ -157,8 +180,12 @@ __global__ __launch_bounds__(kDecide) void reserve_pages(ReserveArgs a) {
 // Forks, first half: which are possible, and which page each one's partly filled page is
 // copied to.  One workgroup, a thread per fork.
 __global__ __launch_bounds__(kDecide) void fork_decide(ForkArgs a) {
-  __shared__ int to[kDecide], fresh[kDecide];
+  __shared__ __attribute__((aligned(16))) int to[kDecide];
+  __shared__ int fresh[kDecide];
+  __shared__ uint16_t list[kDecide * kRun];
   const int i = threadIdx.x;
+  const unsigned ahead =
+      free_mask(a.ref, a.num_blocks, pass_start(a.ref) + (long long)i * kRun);
   const int src = i < a.n ? a.src[i] : -1, dst = i < a.n ? a.dst[i] : -1;
   to[i] = dst;
   __syncthreads();
@@ -168,12 +195,21 @@ __global__ __launch_bounds__(kDecide) void fork_decide(ForkArgs a) {
     kv = a.kv_len[src];
     ok = kv >= 0 && kv <= (a.max_blocks << a.shift) && a.table[(size_t)dst * a.max_blocks] < 0;
   }
-  for (int j = 0; j < a.n; ++j) ok = ok && to[j] != src && (j >= i || to[j] != dst);
+  // (the rest of `to` is -1, which is nobody's number)
+  bool clash = false;
+  for (int j = 0; j < a.n; j += 4) {
+    const int4 t = *(const int4*)(to + j);
+    clash |= t.x == src || t.y == src || t.z == src || t.w == src;
+    clash |= (t.x == dst && j < i) || (t.y == dst && j + 1 < i) || (t.z == dst && j + 2 < i) ||
+             (t.w == dst && j + 3 < i);
+  }
+  ok = ok && !clash;
   const bool part = ok && (kv & ((1 << a.shift) - 1)) != 0;
   int total;
   const int rank = block_scan(part, total);
-  const int found = find_free(a.ref, a.num_blocks, total, [&](int r, int page) { fresh[r] = page; });
-  __syncthreads();
+  const int found = find_free(a.ref, a.num_blocks, total, ahead, list, [&](int r0, int n, int base) {
+    for (int k = i; k < n; k += kDecide) fresh[r0 + k] = base + list[k];
+  });
   if (i >= a.n) return;
   const bool copies = part && rank < found;
   ok = ok && (!part || copies);

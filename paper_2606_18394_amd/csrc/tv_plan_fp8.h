@@ -5,28 +5,41 @@
 
 namespace tv {
 
-// WR x WK waves; units of a key group's ring (8 KB at D = 128, 4 KB at D = 64): 64 KB for
-// every four waves, more does not fit
-constexpr Arrangement kArrangementsFp8[] = {
-    {8, 1, 8, 16}, {4, 2, 8, 16}, {2, 4, 4, 8}, {1, 8, 2, 4}, {4, 1, 8, 16},
+// WR x WK waves of 16 * NT rows each; units of a key group's ring (8 KB at D = 128, 4 KB
+// at D = 64).  A CU holds 8 waves.
+struct ArrangementFp8 {
+  int WR, WK, NT, NU128, NU64;
+};
+constexpr ArrangementFp8 kArrangementsFp8[] = {
+    {1, 8, 1, 2, 4}, {1, 4, 1, 2, 4}, {1, 8, 2, 2, 4}, {1, 4, 2, 2, 4}, {2, 4, 2, 4, 8},
+    {2, 2, 2, 4, 8}, {4, 2, 2, 8, 16}, {4, 1, 2, 8, 16}, {8, 1, 2, 8, 16},
 };
 constexpr int kNumArrangementsFp8 = sizeof(kArrangementsFp8) / sizeof(kArrangementsFp8[0]);
 
+// Dynamic LDS: the rings, then the tree tables; the key-group merge reuses it.
+inline size_t attn_fp8_lds_bytes(const ArrangementFp8& ar, int D, int G, int N) {
+  const int RB = 16 * ar.NT * ar.WR, waves = ar.WR * ar.WK;
+  const size_t ring = (size_t)ar.WK * (D == 128 ? ar.NU128 : ar.NU64) * 64 * D;
+  const size_t tree = (size_t)(RB / G + 2) * cdiv(N, 32) * 4 + (size_t)N * 4 + 16;
+  const size_t merge = ar.WK == 1 ? 0 : (size_t)waves * 16 * ar.NT * (D * 4 + 8);
+  return ring + tree > merge ? ring + tree : merge;
+}
+constexpr size_t kFp8StaticLds = 512;  // what the kernel has beside it, rounded up
+
 inline AttnPlan attn_plan_fp8_arr(int B, int N, int Hq, int Hkv, int D, int Lmax, int arr, long long want) {
-  const Arrangement& ar = kArrangementsFp8[arr];
+  const ArrangementFp8& ar = kArrangementsFp8[arr];
   AttnPlan p{};
   p.arr = arr;
   p.WR = ar.WR;
   p.WK = ar.WK;
-  p.NS = arr_stages(ar, D);
+  p.NS = D == 128 ? ar.NU128 : ar.NU64;
   p.threads = 64 * ar.WR * ar.WK;
   p.G = Hq / Hkv;
   p.wg_per_cu = kWavesPerCU / (ar.WR * ar.WK);
   p.M = N * p.G;
-  p.RB = kRowsPerWave * ar.WR;
+  p.RB = 16 * ar.NT * ar.WR;
   p.nRB = cdiv(p.M, p.RB);
-  // the rings (attn_lds_bytes counts stages of two units), the tree tables, or the merge
-  p.lds_bytes = attn_lds_bytes(D, ar.WR, ar.WK, p.NS / 2, p.G, N, false);
+  p.lds_bytes = attn_fp8_lds_bytes(ar, D, p.G, N);
   const int tiles = cdiv(Lmax, kKeyTile) + cdiv(N, kKeyTile);
   const long long base = (long long)B * Hkv * p.nRB;
   const int min_chunk = 2 * ar.WK;
@@ -52,13 +65,15 @@ inline AttnPlan attn_plan_fp8_arr(int B, int N, int Hq, int Hkv, int D, int Lmax
   return p;
 }
 
+inline bool attn_plan_fp8_fits(const AttnPlan& p) {
+  return (p.lds_bytes + kFp8StaticLds) * p.wg_per_cu <= kMaxLds;
+}
+
 inline AttnPlan attn_plan_fp8(int B, int N, int Hq, int Hkv, int D, int Lmax) {
   const int M = N * (Hq / Hkv);
-  int arr = M <= 32 ? 3 : (M <= 64 ? 2 : (M <= 128 ? 1 : 4));
-  if (attn_plan_fp8_arr(B, N, Hq, Hkv, D, Lmax, arr, B).lds_bytes *
-          (size_t)attn_plan_fp8_arr(B, N, Hq, Hkv, D, Lmax, arr, B).wg_per_cu > kMaxLds)
-    arr = 0;
-  const AttnPlan one = attn_plan_fp8_arr(B, N, Hq, Hkv, D, Lmax, arr, B);
+  int arr = M <= 16 ? 0 : (M <= 32 ? 2 : (M <= 64 ? 4 : (M <= 128 ? 6 : 7)));
+  AttnPlan one = attn_plan_fp8_arr(B, N, Hq, Hkv, D, Lmax, arr, B);
+  if (!attn_plan_fp8_fits(one)) one = attn_plan_fp8_arr(B, N, Hq, Hkv, D, Lmax, arr = 8, B);
   const long long fill = 256LL * one.wg_per_cu / one.nRB / Hkv;
   return fill > B ? attn_plan_fp8_arr(B, N, Hq, Hkv, D, Lmax, arr, fill) : one;
 }

@@ -168,7 +168,7 @@ def test_binding_checks_pages():
     with pytest.raises(ValueError, match="at least one pool"):
         binding.copy_pages(kv, kv, [])
     with pytest.raises(ValueError, match="expected 5 pages"):
-        binding._pool_arrays([torch.zeros(4, 2)], 5, torch.device("cpu"))
+        binding._pool_arrays([torch.zeros(4, 2)], 5, torch.device("cpu"), -1)
     t = _tensors()
     with pytest.raises(ValueError, match="GPU tensor"):
         binding.append_paged_fp8(t["k_tree"], t["v_tree"], t["k_pool"], t["v_pool"], t["k_exp"],
