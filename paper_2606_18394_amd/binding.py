@@ -7,6 +7,7 @@ or the tensors are not on a GPU, the calls raise.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import functools
 import os
@@ -107,7 +108,33 @@ def load_library() -> ctypes.CDLL:
         lib.tv_commit_path_paged.argtypes = (
             [vp, vp, i32p, i32p, vp, vp, i32p] + [ci] * 3 + [i32p] + [ci] * 5 + [vp])
         _lib = lib
+        _connect(lib)
         return lib
+
+
+_direct = None  # the native half of the calls below that have one (csrc/tv_binding.cpp)
+
+
+def _connect(lib) -> None:
+    """Sets up the native half: checks, stream and C entry point of a call in
+    one step, or None where anything is out of the ordinary.  The Python half
+    then does the same and raises what is to be raised; without the native one
+    (not built) it does everything."""
+    global _direct
+    try:
+        from . import _direct as native
+    except ImportError:
+        return
+    native.connect(lib._handle, _raw_stream, getattr(torch._C, "_cuda_getDevice", lambda: -1),
+                   workspace)
+    _direct = native
+
+
+def _current(index):
+    """A context in which device number `index` is the current one."""
+    if torch.cuda.current_device() == index:
+        return contextlib.nullcontext()
+    return torch.cuda.device(index)
 
 
 def status_string(rc: int) -> str:
@@ -323,6 +350,11 @@ def tree_verify_attention_paged_fp8(q, k_pool, v_pool, k_exp, v_exp, block_table
     v_tree, out bf16 as in tree_verify_attention (no tree-tail layout);
     parent [B, N] int32, or None for a chain (N = 1: single-token decoding).
     """
+    if _direct is not None:
+        done = _direct.attention(q, k_pool, v_pool, k_exp, v_exp, block_table, k_tree, v_tree, parent,
+                                 out, kv_len, scale, workspace_tensor)
+        if done is not None:
+            return done
     lib = load_library()
     B, N, Hq, D = qs = q.shape
     Hkv = k_tree.shape[2]
@@ -342,11 +374,12 @@ def tree_verify_attention_paged_fp8(q, k_pool, v_pool, k_exp, v_exp, block_table
     stream = _raw_stream(index)
     need = _bytes("tv_tree_verify_attention_paged_fp8_workspace", B, N, Hq, Hkv, D, mb * bs)
     ws = workspace_tensor if workspace_tensor is not None else workspace("attn", need, dev, stream)
-    rc = lib.tv_tree_verify_attention_paged_fp8(
-        q.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(), k_exp.data_ptr(), v_exp.data_ptr(),
-        block_table.data_ptr(), bs, mb, nb, k_tree.data_ptr(), v_tree.data_ptr(), pp, lp,
-        out.data_ptr(), B, N, Hq, Hkv, D, 0.0 if scale is None else float(scale), ws.data_ptr(),
-        ws.numel(), stream)
+    with _current(index):
+        rc = lib.tv_tree_verify_attention_paged_fp8(
+            q.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(), k_exp.data_ptr(), v_exp.data_ptr(),
+            block_table.data_ptr(), bs, mb, nb, k_tree.data_ptr(), v_tree.data_ptr(), pp, lp,
+            out.data_ptr(), B, N, Hq, Hkv, D, 0.0 if scale is None else float(scale), ws.data_ptr(),
+            ws.numel(), stream)
     if rc:
         _check(rc)
     return out
@@ -358,6 +391,9 @@ def append_paged_fp8(k_new, v_new, k_pool, v_pool, k_exp, v_exp, block_table, kv
     place: rows 0 .. n_new[b] - 1 (n_new None: all) of k_new/v_new
     [B,T,Hkv,D] bf16 become codes and exponents.  kv_len, n_new [B] int32.  A
     sequence without room for its rows is left unchanged."""
+    if _direct is not None and _direct.append(k_new, v_new, k_pool, v_pool, k_exp, v_exp,
+                                              block_table, kv_len, n_new):
+        return
     lib = load_library()
     B, T, Hkv, D = shape = k_new.shape
     dev, index = k_new.device, k_new.get_device()
@@ -369,10 +405,11 @@ def append_paged_fp8(k_new, v_new, k_pool, v_pool, k_exp, v_exp, block_table, kv
         specs += ((n_new, "n_new", _I32, (B,)),)
         rows = n_new.data_ptr()
     _need_all(dev, index, specs)
-    rc = lib.tv_append_paged_fp8(
-        k_new.data_ptr(), v_new.data_ptr(), rows, k_pool.data_ptr(), v_pool.data_ptr(),
-        k_exp.data_ptr(), v_exp.data_ptr(), block_table.data_ptr(), bs, mb, nb, kv_len.data_ptr(), B,
-        T, Hkv, D, _raw_stream(index))
+    with _current(index):
+        rc = lib.tv_append_paged_fp8(
+            k_new.data_ptr(), v_new.data_ptr(), rows, k_pool.data_ptr(), v_pool.data_ptr(),
+            k_exp.data_ptr(), v_exp.data_ptr(), block_table.data_ptr(), bs, mb, nb, kv_len.data_ptr(), B,
+            T, Hkv, D, _raw_stream(index))
     if rc:
         _check(rc)
 
@@ -382,6 +419,9 @@ def commit_path_paged_fp8(k_tree, v_tree, path, accept_len, k_pool, v_pool, k_ex
     """commit_path into a paged cache in 8 bits, in place: the accepted
     path's rows of k_tree/v_tree [B,N,Hkv,D] bf16 are appended as by
     append_paged_fp8.  path [B,Dmax], accept_len [B], kv_len [B] int32."""
+    if _direct is not None and _direct.commit(k_tree, v_tree, path, accept_len, k_pool, v_pool,
+                                              k_exp, v_exp, block_table, kv_len):
+        return
     lib = load_library()
     B, N, Hkv, D = shape = k_tree.shape
     Dmax = path.shape[1]
@@ -391,11 +431,12 @@ def commit_path_paged_fp8(k_tree, v_tree, path, accept_len, k_pool, v_pool, k_ex
         (k_tree, "k_tree", _BF16, shape), (v_tree, "v_tree", _BF16, shape),
         (path, "path", _I32, (B, Dmax)), (accept_len, "accept_len", _I32, (B,)),
         (kv_len, "kv_len", _I32, (B,))) + specs)
-    rc = lib.tv_commit_path_paged_fp8(
-        k_tree.data_ptr(), v_tree.data_ptr(), path.data_ptr(), accept_len.data_ptr(),
-        k_pool.data_ptr(), v_pool.data_ptr(), k_exp.data_ptr(), v_exp.data_ptr(),
-        block_table.data_ptr(), bs, mb, nb, kv_len.data_ptr(), B, N, Hkv, D, Dmax,
-        _raw_stream(index))
+    with _current(index):
+        rc = lib.tv_commit_path_paged_fp8(
+            k_tree.data_ptr(), v_tree.data_ptr(), path.data_ptr(), accept_len.data_ptr(),
+            k_pool.data_ptr(), v_pool.data_ptr(), k_exp.data_ptr(), v_exp.data_ptr(),
+            block_table.data_ptr(), bs, mb, nb, kv_len.data_ptr(), B, N, Hkv, D, Dmax,
+            _raw_stream(index))
     if rc:
         _check(rc)
 
@@ -439,13 +480,18 @@ def reserve_pages(n_rows, block_table, kv_len, ref_count, block_size, ok=None):
     lowest numbers first, go into the rows of block_table in the order of the
     sequences.  Returns ok [B] int32: 0 for a sequence that got none because
     the pages asked for up to it are not there, or because its row has no room."""
+    if _direct is not None and ok is None:
+        done = _direct.reserve(n_rows, block_table, kv_len, ref_count, block_size)
+        if done is not None:
+            return done
     lib = load_library()
     (B, mb, nb, dev, index), specs = _page_state(block_table, ref_count)
     _need_all(dev, index, ((n_rows, "n_rows", _I32, (B,)), (kv_len, "kv_len", _I32, (B,))) + specs)
     ok = _output(ok, "ok", _I32, (B,), dev)
-    rc = lib.tv_reserve_pages(n_rows.data_ptr(), block_table.data_ptr(), kv_len.data_ptr(),
-                              ref_count.data_ptr(), ok.data_ptr(), B, mb, int(block_size), nb,
-                              _raw_stream(index))
+    with _current(index):
+        rc = lib.tv_reserve_pages(n_rows.data_ptr(), block_table.data_ptr(), kv_len.data_ptr(),
+                                  ref_count.data_ptr(), ok.data_ptr(), B, mb, int(block_size), nb,
+                                  _raw_stream(index))
     if rc:
         _check(rc)
     return ok
@@ -458,6 +504,11 @@ def fork_pages(src, dst, block_table, kv_len, ref_count, block_size, pools=(), o
     `pools` ([num_blocks, ...] tensors).  Returns (ok, copy_src, copy_dst) int32
     [n]: whether the fork was made, and the pages copied (-1: none), for
     copy_pages on further pools."""
+    pools = tuple(pools)
+    if _direct is not None and ok is None and copy_src is None and copy_dst is None:
+        done = _direct.fork(src, dst, block_table, kv_len, ref_count, block_size, pools)
+        if done is not None:
+            return done
     lib = load_library()
     (B, mb, nb, dev, index), specs = _page_state(block_table, ref_count)
     n = src.shape[0]
@@ -466,10 +517,11 @@ def fork_pages(src, dst, block_table, kv_len, ref_count, block_size, pools=(), o
     base, size, count = _pool_arrays(pools, nb, dev, index)
     ok, copy_src, copy_dst = _outputs((ok, copy_src, copy_dst), ("ok", "copy_src", "copy_dst"),
                                       ((n,),) * 3, dev)
-    rc = lib.tv_fork_pages(src.data_ptr(), dst.data_ptr(), n, block_table.data_ptr(),
-                           kv_len.data_ptr(), ref_count.data_ptr(), B, mb, int(block_size), nb, base,
-                           size, count, ok.data_ptr(), copy_src.data_ptr(), copy_dst.data_ptr(),
-                           _raw_stream(index))
+    with _current(index):
+        rc = lib.tv_fork_pages(src.data_ptr(), dst.data_ptr(), n, block_table.data_ptr(),
+                               kv_len.data_ptr(), ref_count.data_ptr(), B, mb, int(block_size), nb, base,
+                               size, count, ok.data_ptr(), copy_src.data_ptr(), copy_dst.data_ptr(),
+                               _raw_stream(index))
     if rc:
         _check(rc)
     return ok, copy_src, copy_dst
@@ -478,12 +530,15 @@ def fork_pages(src, dst, block_table, kv_len, ref_count, block_size, pools=(), o
 def free_pages(seqs, block_table, kv_len, ref_count):
     """Sequences seqs (int32 [n]) end: the counts of their pages drop, their
     rows of block_table become empty (-1) and their kv_len 0."""
+    if _direct is not None and _direct.free(seqs, block_table, kv_len, ref_count):
+        return
     lib = load_library()
     (B, mb, nb, dev, index), specs = _page_state(block_table, ref_count)
     n = seqs.shape[0]
     _need_all(dev, index, ((seqs, "seqs", _I32, (n,)), (kv_len, "kv_len", _I32, (B,))) + specs)
-    rc = lib.tv_free_pages(seqs.data_ptr(), n, block_table.data_ptr(), kv_len.data_ptr(),
-                           ref_count.data_ptr(), B, mb, nb, _raw_stream(index))
+    with _current(index):
+        rc = lib.tv_free_pages(seqs.data_ptr(), n, block_table.data_ptr(), kv_len.data_ptr(),
+                               ref_count.data_ptr(), B, mb, nb, _raw_stream(index))
     if rc:
         _check(rc)
 
@@ -498,8 +553,9 @@ def copy_pages(src, dst, pools):
     n, dev, index, nb = src.shape[0], src.device, src.get_device(), pools[0].shape[0]
     _need_all(dev, index, ((src, "src", _I32, (n,)), (dst, "dst", _I32, (n,))))
     base, size, count = _pool_arrays(pools, nb, dev, index)
-    rc = lib.tv_copy_pages(src.data_ptr(), dst.data_ptr(), n, nb, base, size, count,
-                           _raw_stream(index))
+    with _current(index):
+        rc = lib.tv_copy_pages(src.data_ptr(), dst.data_ptr(), n, nb, base, size, count,
+                               _raw_stream(index))
     if rc:
         _check(rc)
 
@@ -522,9 +578,10 @@ def compact_pages(block_table, ref_count, pools=(), n_live=None, copy_src=None, 
     ws = workspace_tensor if workspace_tensor is not None else workspace("pages", need, dev, stream)
     # (a single page cannot move, and its empty lists have no address)
     none = n_live.data_ptr()
-    rc = lib.tv_compact_pages(block_table.data_ptr(), ref_count.data_ptr(), B, mb, nb, base, size,
-                              count, none, copy_src.data_ptr() or none, copy_dst.data_ptr() or none,
-                              ws.data_ptr(), ws.numel(), stream)
+    with _current(index):
+        rc = lib.tv_compact_pages(block_table.data_ptr(), ref_count.data_ptr(), B, mb, nb, base, size,
+                                  count, none, copy_src.data_ptr() or none, copy_dst.data_ptr() or none,
+                                  ws.data_ptr(), ws.numel(), stream)
     if rc:
         _check(rc)
     return n_live, copy_src, copy_dst

@@ -51,6 +51,33 @@ def build(verbose: bool = False) -> str:
     return LIB
 
 
+DIRECT = os.path.join(HERE, "_direct.so")
+
+
+def build_direct(verbose: bool = False, out: str = DIRECT) -> str:
+    """Compile the native half of the binding (host code against torch's
+    headers) into `out`.  Returns the path."""
+    import sysconfig
+
+    import torch
+    root = os.path.dirname(torch.__file__)
+    lib = os.path.join(root, "lib")
+    tmp = out + ".tmp"
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           "-I" + os.path.join(root, "include"),
+           "-I" + os.path.join(root, "include", "torch", "csrc", "api", "include"),
+           "-I" + sysconfig.get_paths()["include"], os.path.join(CSRC, "tv_binding.cpp"), "-o", tmp,
+           "-L" + lib, "-ltorch_python", "-ltorch_cpu", "-ltorch", "-lc10", "-Wl,-rpath," + lib]
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    if res.returncode != 0:
+        raise RuntimeError("g++ failed:\n" + res.stdout + res.stderr)
+    os.replace(tmp, out)
+    return out
+
+
 EXAMPLE_SRC = os.path.join(ROOT, "tests", "native", "abi_example.c")
 EXAMPLE = os.path.join(ROOT, "tests", "native", "abi_example")
 

@@ -176,3 +176,28 @@ def test_binding_checks_pages():
     with pytest.raises(ValueError, match="GPU tensor"):
         binding.commit_path_paged_fp8(t["k_tree"], t["v_tree"], bt, kv, t["k_pool"], t["v_pool"],
                                       t["k_exp"], t["v_exp"], bt, kv)
+
+
+def test_native_half_declines_what_is_not_ordinary():
+    """The native half of the binding answers None for anything that it does not do: tensors of
+    the host, other types, wrong numbers of arguments, things that are no tensors."""
+    _lib()
+    if binding._direct is None:
+        from paper_2606_18394_amd import build
+        build.build_direct()
+        binding._connect(binding.load_library())
+    d, t = binding._direct, _tensors()
+    i32 = torch.int32
+    bt, kv, ref = torch.zeros(2, 3, dtype=i32), torch.zeros(2, dtype=i32), torch.zeros(5, dtype=i32)
+    cache = [t[k] for k in ("k_pool", "v_pool", "k_exp", "v_exp", "block_table")]
+    calls = [(d.attention, [t["q"]] + cache + [t["k_tree"], t["v_tree"], t["parent"], t["out"], kv, None, None]),
+             (d.append, [t["k_tree"], t["v_tree"]] + cache + [kv, None]),
+             (d.commit, [t["k_tree"], t["v_tree"], bt, kv] + cache + [kv]),
+             (d.reserve, [kv, bt, kv, ref, 64]), (d.fork, [kv, kv, bt, kv, ref, 64, ()]),
+             (d.free, [kv, bt, kv, ref])]
+    for call, args in calls:
+        assert call(*args) is None
+        assert call() is None and call(*args[:-1]) is None
+        for i in range(len(args)):
+            for other in (None, 7, "x", torch.zeros(3)):
+                assert call(*args[:i], other, *args[i + 1:]) is None
