@@ -429,8 +429,8 @@ void attn_fp8(Fp8Args a) {
 
   const bool busy = wrow0 < a.M;  // else only the tiles are moved
   uint32_t bits[NT] = {};
-  int head = 0;  // the next step's first unit
-  auto refill = [&]() {  // into what the steps before `head` took up
+  int head = 0;  // units taken so far
+  auto refill = [&]() {  // in the place of the units before `head`
     while (issued < n_units && issued < head + NU) {
       if (issued < n_c && (issued & 63) == 0) {
         group = group_of(issued);
@@ -440,18 +440,18 @@ void attn_fp8(Fp8Args a) {
       ++issued;
     }
   };
-  // Step i: its units are there once at most the later ones' DMAs are in flight; the
-  // barrier makes the whole group's visible, and what the steps before took up is free.
-  auto ring_step = [&](int i) {
-    const bool mine = i < n_mine;
-    const int next = head + (mine ? (i < n_c ? 1 : 2) : 0);
-    if (kAlone) {
-      if (mine) wait_tiles<PU, NU>(issued - next);
-    } else {
-      if (mine && mover) wait_tiles<PU, NU>(issued - next);
+  // Waits for the units before `next`, which are there once at most the later ones' DMAs
+  // are in flight.  In a shared ring the barrier makes the whole group's visible, and the
+  // units that were taken before it are done with: their places are filled again.
+  auto arrive = [&](int next) {
+    if (next > head && mover) wait_tiles<PU, NU>(issued - next);
+    if (!kAlone) {
       __syncthreads();
-      if (i > 0) refill();
+      refill();
     }
+    head = next;
+  };
+  auto exponents = [&](int i) {  // of tile i and the ones after it, every 64 tiles
     if (i > 0 && i < n_c && (i & 63) == 0) {
       const int at = group_of(i);
       kexp = a.ke[at];
@@ -459,7 +459,6 @@ void attn_fp8(Fp8Args a) {
       loaded(kexp);
       loaded(vexp);
     }
-    head = next;
   };
   // A wave alone frees a cache tile's place as soon as it holds the codes.
   Codes<D> codes;
@@ -474,20 +473,35 @@ void attn_fp8(Fp8Args a) {
   auto scale_of = [&](int exps, int i) {
     return __int_as_float(__builtin_amdgcn_readlane(exps, i & 63) << 23);
   };
-  // Full cache tiles first, without masking, then the cache's tail and the tree.
+  // Full cache tiles first, without masking.  Waves that share a ring meet once for half
+  // of it, not at every tile: between two meetings they drift apart, so that one's matrix
+  // work falls on the other's vector work.
+  constexpr int kMeet = kAlone ? 1 : NU / 2;
+  static_assert(64 % kMeet == 0, "exponents are looked up where waves meet");
+  auto full_tiles = [&](int k) {  // of key group k
+    return max(0, (min(t1, kvl / kKeyTile) - t0 - k + WK - 1) / WK);
+  };
+  const int n_full = full_tiles(wk);
+  const int n_meet = kAlone ? n_full : (full_tiles(0) + kMeet - 1) / kMeet;  // the same for all groups
   int i = 0;
-  for (; i < n_iter; ++i) {
-    if (i >= n_c || (t0 + wk + WK * i + 1) * kKeyTile > kvl) break;
-    const uint32_t unit = ring + (head % NU) * UNIT;
-    ring_step(i);
-    if (!busy) continue;
-    take(unit, g4, l16);
-    attend_codes<D, NT, false, kAlone>(codes, unit, scale_of(kexp, i), scale_of(vexp, i), qf, o, lacc, m,
-                                       thr, ones, a.c, inv_c, bits, g4, l16);
+  for (int k = 0; k < n_meet; ++k) {
+    const int end = min(n_full, (k + 1) * kMeet);
+    arrive(max(end, head));
+    exponents(i);
+    for (; i < end && busy; ++i) {
+      const uint32_t unit = ring + (i % NU) * UNIT;
+      take(unit, g4, l16);
+      attend_codes<D, NT, false, kAlone>(codes, unit, scale_of(kexp, i), scale_of(vexp, i), qf, o, lacc, m,
+                                         thr, ones, a.c, inv_c, bits, g4, l16);
+    }
   }
-  for (; i < n_iter; ++i) {
+  // Then the cache's tail and the tree, tile by tile (as many steps for all groups).
+  const int n_rest = kAlone ? n_mine - n_full : n_iter - full_tiles(WK - 1);
+  for (int k = 0; k < n_rest; ++k) {
+    i = n_full + k;
     const int at = (head % NU) * UNIT, at_v = ((head + 1) % NU) * UNIT;
-    ring_step(i);
+    arrive(head + (i < n_mine ? (i < n_c ? 1 : 2) : 0));
+    exponents(i);
     if (i >= n_mine || !busy) continue;
     // (opaque lane numbers: the addresses of these few tiles' reads are not kept through
     // the loop above)
@@ -499,7 +513,8 @@ void attn_fp8(Fp8Args a) {
       attend_codes<D, NT, true, kAlone>(codes, ring + at, scale_of(kexp, i), scale_of(vexp, i), qf, o, lacc,
                                         m, thr, ones, a.c, inv_c, bits, hg4, hl16);
     } else {
-      attend_tree<D, NT>(ring_ptr + at, ring_ptr + at_v, qf, o, lacc, m, thr, ones, a.c, inv_c, bits, hg4, hl16);
+      attend_tree<D, NT>(ring_ptr + at, ring_ptr + at_v, qf, o, lacc, m, thr, ones, a.c, inv_c, bits, hg4,
+                         hl16);
       if (kAlone) refill();
     }
   }
