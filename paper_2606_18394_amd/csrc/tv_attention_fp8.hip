@@ -229,10 +229,12 @@ void attn_fp8(Fp8Args a) {
   static_assert(NU >= 2, "a tree tile is two units");
   extern __shared__ __attribute__((aligned(128))) unsigned char smem[];
 
-  // The work item, as in attn_main.
+  // The work item: one of the even split, which goes by the kv_lens, or (unsplit) one that
+  // is known at once, with the sequence's length still on its way.
   WorkItem it{};
-  int chunk = a.chunk, kvl, part0;  // part0: the row block's first chunk partial
-  if (a.slots > 0) {
+  int chunk = a.chunk, kvl = 0, asked = 0, part0 = 0;  // part0: the row block's first chunk partial
+  const bool split = a.slots > 0;
+  if (split) {
     const int item = even_item(blockIdx.x, a.slots, a.nRB, a.Hkv, it);
     if (item < 0) return;
     const EvenItem ev = even_split<false>(a, item, 0, 0);
@@ -244,22 +246,72 @@ void attn_fp8(Fp8Args a) {
     part0 = (it.g * a.nRB + it.rb) * a.slots + ev.first;
   } else {
     if (!work_item(gridDim.x, a.nwork, a.S, a.nRB, 0, a.B, a.Hkv, blockIdx.x, it)) return;
-    kvl = context_rows(a, it.b);
-    part0 = ((it.b * a.Hkv + it.g) * a.nRB + it.rb) * a.S;
+    if (a.kv_len) asked = a.kv_len[it.b];
   }
   const int s = it.s, rb = it.rb, g = it.g, b = it.b;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wr = wave % WR, wk = wave / WR;
   const int g4 = lane >> 4, l16 = lane & 15;
-
   const int r0 = rb * RB;
   const int rows = min(RB, a.M - r0);
   const int i_lo = r0 / a.G, i_hi = (r0 + rows - 1) / a.G;
+  const int ntt = i_hi / kKeyTile + 1;  // words of a node's ancestor bitmask
+  const int t0 = s * chunk;
+
+  // All that does not hang on the length is asked for before it is there: parents (of up
+  // to 32 nodes every wave has its own, else the workgroup shares them), queries, and
+  // the places of the first tiles.  One round trip to memory less: a single token over
+  // 200 rows 6.7 -> 6.0 us.
+  const bool small = a.N <= 32;
+  constexpr int kParPerThread = (kMaxNodes + kThreads - 1) / kThreads;
+  constexpr int NQ = NT * NC;  // query loads per lane
+  int pv[kParPerThread];
+  const int32_t* pr = a.parent ? a.parent + (size_t)b * a.N : (const int32_t*)a.q;  // NULL: a chain
+  int own_parent = load_i32(pr + (a.parent && lane < a.N ? lane : 0));
+  if (!small) {
+    // indices clamped rather than branched on, so the loads stay in flight
+#pragma unroll
+    for (int k = 0; k < kParPerThread; ++k) {
+      const int i = tid + kThreads * k;
+      pv[k] = load_i32(pr + (!a.parent ? 0 : i < a.N ? i : a.N - 1));
+    }
+  }
+  // ---- queries: B operand of S^T = K Q^T
+  const int wrow0 = r0 + kRows * wr;
+  bf16x8 qf[NT][NC];
+  bool qok[NT];
+  int node_of[NT];  // this lane's row's, of the last row past it
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const int r = wrow0 + nt * 16 + l16;
+    const int in = min(r, a.M - 1);
+    qok[nt] = r < a.M;
+    node_of[nt] = in / a.G;
+    const int h = g * a.G + in % a.G;
+    const __bf16* qp = a.q + ((size_t)(b * a.N + node_of[nt]) * a.Hq + h) * D + head_dim(0, g4);
+#pragma unroll
+    for (int cc = 0; cc < NC; ++cc) qf[nt][cc] = load_b128(qp + head_dim(cc, 0));
+  }
+  // Tile i0 + lane's place in the pools, in groups (of tiles past the cache's, or the
+  // capacity, somewhere in the pool).  Block numbers are clamped into the pool.
+  auto group_of = [&](int i0) {
+    const int first = min((t0 + wk + WK * (i0 + lane)) * kKeyTile, a.Lmax - kKeyTile);
+    const int blk = a.block_table[(size_t)b * a.max_blocks + (first >> a.block_shift)];
+    const int page = min(max(blk, 0), a.num_blocks - 1), per = a.block_shift - 5;
+    return ((page * a.Hkv + g) << per) + ((first >> 5) & ((1 << per) - 1));
+  };
+  int group = 0;  // of tiles 64 j + lane, j that of the tile issued last
+  if (a.Lmax > 0) group = group_of(0);
+  // exponents of tiles 64 j + lane, j that of the tile attended to (without a cache
+  // anything that may be read: the loads are counted below)
+  int kexp = load_u8(a.Lmax > 0 ? a.ke + group : (const uint8_t*)a.q);
+  int vexp = load_u8(a.Lmax > 0 ? a.ve + group : (const uint8_t*)a.q);
+
+  if (!split) kvl = context_rows_of(a, asked);
   const Segment sg = segment(a, kvl, i_hi);
   const int nct = sg.nct, T = sg.T;
-  const int ntt = i_hi / kKeyTile + 1;  // words of a node's ancestor bitmask
-  const int t0 = s * chunk, t1 = min(T, t0 + chunk);
+  const int t1 = min(T, t0 + chunk);
   if (t0 >= t1) return;  // empty chunk: the merge reads only chunks with tiles
   const bool has_tree = t1 > nct;
 
@@ -267,7 +319,7 @@ void attn_fp8(Fp8Args a) {
   const unsigned char* ring_ptr = smem + wk * NU * UNIT;
   uint32_t* anc = reinterpret_cast<uint32_t*>(smem + WK * NU * UNIT);  // behind the rings
   int32_t* par = reinterpret_cast<int32_t*>(anc + (RB / a.G + 2) * ntt);
-  int* flag = par + a.N;
+  __shared__ unsigned long long brk[kMaxNodes / 64];
 
   // The key group's tiles are t0 + wk + WK * i, n_mine of them, the first n_c the cache's.
   // All waves take n_iter steps, so that the steps' barriers line up.
@@ -275,52 +327,6 @@ void attn_fp8(Fp8Args a) {
   const int n_mine = t0 + wk < t1 ? (t1 - t0 - wk + WK - 1) / WK : 0;
   const int n_c = max(0, (min(t1, nct) - t0 - wk + WK - 1) / WK);
   const int n_units = 2 * n_mine - n_c;
-
-  // Tile i0 + lane's place in the pools, in groups.  Block numbers are clamped into the
-  // pool.
-  auto group_of = [&](int i0) {
-    const int first = (t0 + wk + WK * min(i0 + lane, n_c - 1)) * kKeyTile;
-    const int blk = a.block_table[(size_t)b * a.max_blocks + (first >> a.block_shift)];
-    const int page = min(max(blk, 0), a.num_blocks - 1), per = a.block_shift - 5;
-    return ((page * a.Hkv + g) << per) + ((first >> 5) & ((1 << per) - 1));
-  };
-  int group = 0;  // of tiles 64 j + lane, j that of the tile issued last
-  if (n_c > 0) group = group_of(0);
-
-  // Parents, queries, exponents and the first units are all requested before any is used.
-  constexpr int kParPerThread = (kMaxNodes + kThreads - 1) / kThreads;
-  constexpr int NQ = NT * NC;  // query loads per lane
-  int pv[kParPerThread];
-  if (has_tree) {
-    // indices clamped rather than branched on, so the loads stay in flight
-    const int32_t* pr = a.parent + (size_t)b * a.N;
-#pragma unroll
-    for (int k = 0; k < kParPerThread; ++k) {
-      const int i = tid + kThreads * k;
-      pv[k] = a.parent ? load_i32(pr + (i < a.N ? i : a.N - 1)) : i - 1;  // NULL: a chain
-    }
-  }
-
-  // ---- queries: B operand of S^T = K Q^T
-  const int wrow0 = r0 + kRows * wr;
-  bf16x8 qf[NT][NC];
-  bool qok[NT];
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    const int r = wrow0 + nt * 16 + l16;
-    const bool ok = r < a.M;
-    qok[nt] = ok;
-    const int node = ok ? r / a.G : 0;
-    const int h = g * a.G + (ok ? r % a.G : 0);
-    const __bf16* qp = a.q + ((size_t)(b * a.N + node) * a.Hq + h) * D + head_dim(0, g4);
-#pragma unroll
-    for (int cc = 0; cc < NC; ++cc) qf[nt][cc] = load_b128(qp + head_dim(cc, 0));
-  }
-
-  // exponents of tiles 64 j + lane, j that of the tile attended to (without a cache tile
-  // anything that may be read: the loads are counted below)
-  int kexp = load_u8(n_c > 0 ? a.ke + group : (const uint8_t*)a.q);
-  int vexp = load_u8(n_c > 0 ? a.ve + group : (const uint8_t*)a.q);
 
   const size_t krow = (size_t)a.Hkv * D;  // the tree's: elements between consecutive nodes
   const size_t tree0 = ((size_t)b * a.N * a.Hkv + g) * D;
@@ -364,36 +370,72 @@ void attn_fp8(Fp8Args a) {
   if (mover)
     for (int u = 0; u < issued; ++u) issue_unit(u);
 
-  // ---- tree structure: ancestor-or-self bitmask of this block's nodes
-  if (has_tree) {
-    // the parents are done once at most queries, exponents and DMAs are in flight
-    wait_vm_any(NQ + 2 + in_flight);
+  // ---- tree structure: which nodes are a node's ancestors or itself, as bits
+  int invalid = 0;
+  // of this lane's rows: the nodes relative to i_lo, in small trees what they see of it
+  int node_rel[NT];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) node_rel[nt] = node_of[nt] - i_lo;
+  // the parents are done once at most queries, exponents and DMAs are in flight
+  wait_vm_any(NQ + 2 + in_flight);
+  loaded(own_parent);
+  if (has_tree && small) {
+    // node `lane`: twice as far up with every step
+    const int p = a.parent ? own_parent : lane - 1;
+    const bool in = lane < a.N;
+    invalid = __any(in && (lane == 0 ? p != -1 : p < 0 || p >= lane));
+    uint32_t up = in ? 1u << lane : 0u;
+    int to = in && lane > 0 && !invalid ? p : lane;
+    for (int far = 1; far < a.N; far *= 2) {
+      up |= __shfl(up, to);
+      to = __shfl(to, to);
+    }
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) node_rel[nt] = __shfl((int)up, node_of[nt]);
+  }
+  if (!small) {
 #pragma unroll
     for (int k = 0; k < kParPerThread; ++k) loaded(pv[k]);
-    int bad = 0;
+  }
+  if (has_tree && !small) {
 #pragma unroll
     for (int k = 0; k < kParPerThread; ++k) {
       const int i = tid + kThreads * k;
-      if (i >= a.N) break;
-      const int p = pv[k];
-      par[i] = p;
-      bad |= (i == 0) ? (p != -1) : (p < 0 || p >= i);
+      const int p = a.parent ? pv[k] : i - 1;
+      const bool in = i < a.N;
+      if (in) par[i] = p;
+      invalid |= in && ((i == 0) ? (p != -1) : (p < 0 || p >= i));
+      // nodes whose parent is not the node before them
+      const unsigned long long breaks = __ballot(in && p != i - 1);
+      if (lane == 0 && in) brk[i >> 6] = breaks;
     }
-    bad = __syncthreads_or(bad);
+    invalid = __syncthreads_or(invalid);
+    // Up from node to node; after some steps, which end what drafts are usually like, a
+    // run of nodes that follow their parents at a time (of a chain 64: step by step a
+    // chain of 269 nodes took 30 us; 86 nodes of depth 12 by runs alone 1 us more).
     const int nodes = i_hi - i_lo + 1;
     for (int t = tid; t < nodes; t += kThreads) {
       uint32_t* wd = anc + t * ntt;
       for (int k = 0; k < ntt; ++k) wd[k] = 0u;
       int u = i_lo + t;
-      for (;;) {
+      for (int steps = 0; steps < 16 && u > 0; ++steps) {
         wd[u >> 5] |= 1u << (u & 31);
-        if (u == 0) break;
         const int p = par[u];
-        if (p < 0 || p >= u) break;  // invalid tree: the output becomes NaN
+        u = p >= 0 && p < u ? p : -1;  // invalid tree: the output becomes NaN
+      }
+      while (u >= 0) {
+        const int base = u & ~63;
+        const unsigned long long m = brk[u >> 6] & (~0ull >> (63 - (u & 63)));
+        const int top = m ? base + 63 - __clzll((long long)m) : base;  // the run's first node
+        const unsigned long long run = (~0ull >> (63 - (u - top))) << (top & 63);
+        wd[base >> 5] |= (uint32_t)run;
+        if ((base >> 5) + 1 < ntt) wd[(base >> 5) + 1] |= (uint32_t)(run >> 32);
+        if (top == 0) break;
+        const int p = m ? par[top] : top - 1;
+        if (p < 0 || p >= top) break;  // invalid tree: the output becomes NaN
         u = p;
       }
     }
-    if (tid == 0) *flag = bad;
     __syncthreads();
   }
 
@@ -412,15 +454,12 @@ void attn_fp8(Fp8Args a) {
   // O^T accumulators, and the row sums of the rounded weights as ones^T P^T
   f32x4 o[DT][NT], lacc[NT];
   float m[NT], thr[NT];
-  int node_rel[NT];  // node of this lane's row in each 16-row tile, relative to i_lo
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     m[nt] = thr[nt] = -INFINITY;
     lacc[nt] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) o[dt][nt] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const int r = wrow0 + nt * 16 + l16;
-    node_rel[nt] = (r < a.M ? r : a.M - 1) / a.G - i_lo;
   }
   bf16x8 ones = {(__bf16)1.f, (__bf16)1.f, (__bf16)1.f, (__bf16)1.f,
                  (__bf16)1.f, (__bf16)1.f, (__bf16)1.f, (__bf16)1.f};
@@ -507,7 +546,12 @@ void attn_fp8(Fp8Args a) {
     // the loop above)
     int hg4 = g4, hl16 = l16;
     asm volatile("" : "+v"(hg4), "+v"(hl16));
-    tile_bits<NT>(MaskInfo{t0 + wk + WK * i, nct, kvl, ntt, 0, anc}, node_rel, bits);
+    if (i < n_c || !small) {
+      tile_bits<NT>(MaskInfo{t0 + wk + WK * i, nct, kvl, ntt, 0, anc}, node_rel, bits);
+    } else {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) bits[nt] = (uint32_t)node_rel[nt];
+    }
     if (i < n_c) {
       take(ring + at, hg4, hl16);
       attend_codes<D, NT, true, kAlone>(codes, ring + at, scale_of(kexp, i), scale_of(vexp, i), qf, o, lacc,
@@ -523,7 +567,6 @@ void attn_fp8(Fp8Args a) {
   float lsum[NT];
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) lsum[nt] = lacc[nt][0];
-  const int invalid = has_tree ? *flag : 0;
   // A row block that is one chunk writes its output here, else its partial; fragments
   // wholly past the last row are neither stored nor read by the merges.
   const int nval = (T + chunk - 1) / chunk;

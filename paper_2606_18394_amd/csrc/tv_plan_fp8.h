@@ -11,8 +11,8 @@ struct ArrangementFp8 {
   int WR, WK, NT, NU128, NU64;
 };
 constexpr ArrangementFp8 kArrangementsFp8[] = {
-    {1, 8, 1, 2, 4}, {1, 4, 1, 2, 4}, {1, 8, 2, 2, 4}, {1, 4, 2, 2, 4}, {2, 4, 2, 4, 8},
-    {2, 2, 2, 4, 8}, {4, 2, 2, 8, 16}, {4, 1, 2, 8, 16}, {8, 1, 2, 8, 16},
+    {1, 8, 1, 2, 4}, {1, 4, 1, 2, 4}, {1, 8, 2, 2, 4}, {1, 4, 2, 2, 4}, {2, 4, 2, 4, 8}, {2, 2, 2, 4, 8},
+    {4, 1, 2, 8, 16},
 };
 constexpr int kNumArrangementsFp8 = sizeof(kArrangementsFp8) / sizeof(kArrangementsFp8[0]);
 
@@ -24,7 +24,7 @@ inline size_t attn_fp8_lds_bytes(const ArrangementFp8& ar, int D, int G, int N) 
   const size_t merge = ar.WK == 1 ? 0 : (size_t)waves * 16 * ar.NT * (D * 4 + 8);
   return ring + tree > merge ? ring + tree : merge;
 }
-constexpr size_t kFp8StaticLds = 512;  // what the kernel has beside it, rounded up
+constexpr size_t kFp8StaticLds = 1024;  // what the kernel has beside it, rounded up
 
 inline AttnPlan attn_plan_fp8_arr(int B, int N, int Hq, int Hkv, int D, int Lmax, int arr, long long want) {
   const ArrangementFp8& ar = kArrangementsFp8[arr];
@@ -71,9 +71,8 @@ inline bool attn_plan_fp8_fits(const AttnPlan& p) {
 
 inline AttnPlan attn_plan_fp8(int B, int N, int Hq, int Hkv, int D, int Lmax) {
   const int M = N * (Hq / Hkv);
-  int arr = M <= 16 ? 0 : (M <= 32 ? 2 : (M <= 64 ? 4 : (M <= 128 ? 6 : 7)));
+  int arr = M <= 16 ? 0 : (M <= 32 ? 2 : (M <= 64 ? 4 : 6));
   AttnPlan one = attn_plan_fp8_arr(B, N, Hq, Hkv, D, Lmax, arr, B);
-  if (!attn_plan_fp8_fits(one)) one = attn_plan_fp8_arr(B, N, Hq, Hkv, D, Lmax, arr = 8, B);
   const long long fill = 256LL * one.wg_per_cu / one.nRB / Hkv;
   return fill > B ? attn_plan_fp8_arr(B, N, Hq, Hkv, D, Lmax, arr, fill) : one;
 }
