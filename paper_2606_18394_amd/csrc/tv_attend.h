@@ -146,28 +146,6 @@ __device__ __forceinline__ void longest_first(const AttnArgs& a, int bid, WorkIt
   it.s = chunk_of(p, it.b);
 }
 
-__device__ __forceinline__ int wave_sum(int x) {
-  x += (int)dpp_u32<0xB1>((unsigned)x);
-  x += (int)dpp_u32<0x4E>((unsigned)x);
-  x += (int)dpp_u32<0x141>((unsigned)x);
-  x += (int)dpp_u32<0x140>((unsigned)x);
-  return __builtin_amdgcn_readlane(x, 0) + __builtin_amdgcn_readlane(x, 16) +
-         __builtin_amdgcn_readlane(x, 32) + __builtin_amdgcn_readlane(x, 48);
-}
-
-// Sums over the lanes up to each one (shifts by 1, 2, 4 and 8 lanes inside a
-// row of 16, then row 0's and row 2's last lane into the next row and lane 31
-// into rows 2 and 3), without the LDS crossbar.
-__device__ __forceinline__ int wave_scan(int x) {
-  x += (int)dpp_u32<0x111>((unsigned)x);
-  x += (int)dpp_u32<0x112>((unsigned)x);
-  x += (int)dpp_u32<0x114>((unsigned)x);
-  x += (int)dpp_u32<0x118>((unsigned)x);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);
-  return x;
-}
-
 // ceil(x / c) for 0 <= x < 2^20, 1 <= c < 2^20, rc = 1 / c to one ulp: the
 // quotient's distance to the next whole number below, at least 1 / (2 c), is
 // above the errors of the reciprocal and the product (together 1.5 * 2^-23 of a

@@ -14,6 +14,7 @@
 #include <stdint.h>
 
 #include "tv_pages.h"
+#include "tv_walk.h"
 
 namespace tv {
 
@@ -21,24 +22,22 @@ typedef int i32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kDecide = 1024;  // threads of a deciding workgroup
 
-// Sum of x over the workgroup's threads before this one, and over all of them.
+// Sum of x over the workgroup's (kDecide) threads before this one, and over all of them.
 __device__ __forceinline__ int block_scan(int x, int& total) {
-  __shared__ int sums[kDecide / 64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = (blockDim.x + 63) / 64;
-  int upto = x;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int y = __shfl_up(upto, d);
-    if (lane >= d) upto += y;
-  }
+  constexpr int kWaves = kDecide / 64;
+  __shared__ __attribute__((aligned(16))) int sums[kWaves];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int upto = wave_scan(x);
   __syncthreads();  // the sums of a call before this one are read
   if (lane == 63) sums[wave] = upto;
   __syncthreads();
   int before = 0;
   total = 0;
-  for (int w = 0; w < waves; ++w) {
-    if (w == wave) before = total;
-    total += sums[w];
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    const int n = sums[w];
+    before += w < wave ? n : 0;
+    total += n;
   }
   return before + upto - x;
 }
@@ -304,7 +303,7 @@ __global__ __launch_bounds__(kCopyThreads) void copy_pages(CopyArgs a) {
 // Compaction.  With L live pages, free pages below L and live ones from L on are equally
 // many; the d-th such free page (upwards) takes the d-th such live one (downwards).  With
 // P(x) live pages below x: free x < L has d = x - P(x), live x >= L has d = L - 1 - P(x).
-// Three kernels: counts per run of pages; places; then copies, counts and tables.
+// Kernels: counts per run of pages; places; then copies, counts and tables.
 __device__ __forceinline__ unsigned live_of(const CompactArgs& a, long long first, int& n) {
   unsigned live = 0;
   n = 0;
@@ -315,12 +314,7 @@ __device__ __forceinline__ unsigned live_of(const CompactArgs& a, long long firs
   return live;
 }
 
-__global__ __launch_bounds__(kDecide) void compact_count(CompactArgs a) {
-  const long long first = ((long long)blockIdx.x * kDecide + threadIdx.x) * kCompactPer;
-  int n, total;
-  live_of(a, first, n);
-  block_scan(n, total);
-  if (threadIdx.x == 0) a.counts[blockIdx.x] = total;
+__device__ __forceinline__ void clear_lists(const CompactArgs& a, long long first) {
   for (int k = 0; k < kCompactPer; ++k) {
     const long long x = first + k;
     if (x < a.num_blocks) a.place[x] = -1;
@@ -328,22 +322,34 @@ __global__ __launch_bounds__(kDecide) void compact_count(CompactArgs a) {
   }
 }
 
-__global__ __launch_bounds__(kDecide) void compact_place(CompactArgs a) {
-  const int runs = gridDim.x;
-  int before = 0, all = 0, sum;
-  for (int r = threadIdx.x; r < runs; r += kDecide) {
-    const int c = a.counts[r];
-    all += c;
-    before += r < (int)blockIdx.x ? c : 0;
-  }
-  block_scan(before, sum);
-  before = sum;
-  block_scan(all, sum);
-  const int L = sum;
+__global__ __launch_bounds__(kDecide) void compact_count(CompactArgs a) {
   const long long first = ((long long)blockIdx.x * kDecide + threadIdx.x) * kCompactPer;
   int n, total;
+  live_of(a, first, n);
+  block_scan(n, total);
+  if (threadIdx.x == 0) a.counts[blockIdx.x] = total;
+  clear_lists(a, first);
+}
+
+// (A single run is counted here: a kernel less, 5 us.)
+__global__ __launch_bounds__(kDecide) void compact_place(CompactArgs a) {
+  const int runs = gridDim.x;
+  const long long first = ((long long)blockIdx.x * kDecide + threadIdx.x) * kCompactPer;
+  int n, L, before = 0, sum;
   const unsigned live = live_of(a, first, n);
-  int P = before + block_scan(n, total);
+  if (runs == 1) clear_lists(a, first);
+  int P = block_scan(n, L);  // (its barriers: the lists are cleared)
+  if (runs > 1) {
+    int all = 0;
+    for (int r = threadIdx.x; r < runs; r += kDecide) {
+      const int c = a.counts[r];
+      all += c;
+      before += r < (int)blockIdx.x ? c : 0;
+    }
+    block_scan(before, sum);
+    P += sum;
+    block_scan(all, L);
+  }
   for (int k = 0; k < kCompactPer; ++k) {
     const long long x = first + k;
     if (x >= a.num_blocks) break;
@@ -421,9 +427,11 @@ hipError_t launch_copy(const CopyArgs& a, hipStream_t st) {
 
 hipError_t launch_compact(const CompactArgs& a, hipStream_t st) {
   const dim3 runs((unsigned)compact_runs(a.num_blocks));
-  hipLaunchKernelGGL(compact_count, runs, dim3(kDecide), 0, st, a);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
+  hipError_t e = hipSuccess;
+  if (runs.x > 1) {
+    hipLaunchKernelGGL(compact_count, runs, dim3(kDecide), 0, st, a);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
   hipLaunchKernelGGL(compact_place, runs, dim3(kDecide), 0, st, a);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   const long long items = (long long)(a.num_blocks / 2) * a.pools.total;

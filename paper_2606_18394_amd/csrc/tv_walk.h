@@ -1,6 +1,6 @@
-// Device helpers shared by the greedy and the non-greedy tree acceptance:
+// Device helpers shared by the greedy and the non-greedy tree acceptance and others:
 // the pointer-jumping state of one node packed into a 32-bit word, and
-// wave-wide unsigned maxima on DPP exchanges.  Pointer jumping over the parent links finds,
+// wave-wide unsigned maxima, sums and scans on DPP exchanges.  Pointer jumping over the parent links finds,
 // for every node at once, its depth and whether every node on its root path
 // passed its test, in O(log depth) rounds.
 #pragma once
@@ -59,6 +59,28 @@ __device__ __forceinline__ unsigned int wave_max_u32(unsigned int x) {
   x = max(x, dpp_bcast_u32<0x142, 0xA>(x));
   x = max(x, dpp_bcast_u32<0x143, 0xC>(x));
   return __builtin_amdgcn_readlane(x, 63);
+}
+
+__device__ __forceinline__ int wave_sum(int x) {
+  x += (int)dpp_u32<0xB1>((unsigned)x);
+  x += (int)dpp_u32<0x4E>((unsigned)x);
+  x += (int)dpp_u32<0x141>((unsigned)x);
+  x += (int)dpp_u32<0x140>((unsigned)x);
+  return __builtin_amdgcn_readlane(x, 0) + __builtin_amdgcn_readlane(x, 16) +
+         __builtin_amdgcn_readlane(x, 32) + __builtin_amdgcn_readlane(x, 48);
+}
+
+// Sums over the lanes up to each one (shifts by 1, 2, 4 and 8 lanes inside a
+// row of 16, then row 0's and row 2's last lane into the next row and lane 31
+// into rows 2 and 3), without the LDS crossbar.
+__device__ __forceinline__ int wave_scan(int x) {
+  x += (int)dpp_u32<0x111>((unsigned)x);
+  x += (int)dpp_u32<0x112>((unsigned)x);
+  x += (int)dpp_u32<0x114>((unsigned)x);
+  x += (int)dpp_u32<0x118>((unsigned)x);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);
+  return x;
 }
 
 }  // namespace tv
