@@ -69,7 +69,8 @@ static_assert(TV_MAX_WIDTH == tv::kTopwMax, "width limit mismatch");
 // and each needs its plan twice (workspace size, launch), so every thread keeps
 // the last one: the search over the arrangements takes about as long as a
 // launch.
-static const tv::AttnPlan& attn_plan_of(int B, int N, int Hq, int Hkv, int D, int Lmax) {
+template <tv::AttnPlan (*search)(int, int, int, int, int, int)>
+static const tv::AttnPlan& last_plan(int B, int N, int Hq, int Hkv, int D, int Lmax) {
   struct Last {
     int key[6];
     tv::AttnPlan plan;
@@ -77,10 +78,13 @@ static const tv::AttnPlan& attn_plan_of(int B, int N, int Hq, int Hkv, int D, in
   static thread_local Last last = {};
   const int key[6] = {B, N, Hq, Hkv, D, Lmax};
   if (memcmp(key, last.key, sizeof key) != 0) {
-    last.plan = tv::attn_plan(B, N, Hq, Hkv, D, Lmax);
+    last.plan = search(B, N, Hq, Hkv, D, Lmax);
     memcpy(last.key, key, sizeof key);
   }
   return last.plan;
+}
+static const tv::AttnPlan& attn_plan_of(int B, int N, int Hq, int Hkv, int D, int Lmax) {
+  return last_plan<tv::attn_plan>(B, N, Hq, Hkv, D, Lmax);
 }
 
 // The plan that a call's workspace allows; ok: there is one.
@@ -276,7 +280,7 @@ static int check_pages_fp8(int Hkv, int block_size, int max_blocks, int num_bloc
 
 size_t tv_tree_verify_attention_paged_fp8_workspace(int B, int N, int Hq, int Hkv, int D, int Lmax) {
   if (check_attention_sizes(B, N, Hq, Hkv, D, Lmax) != TV_OK) return 0;
-  const size_t need = tv::attn_plan_fp8(B, N, Hq, Hkv, D, Lmax).ws_bytes;
+  const size_t need = last_plan<tv::attn_plan_fp8>(B, N, Hq, Hkv, D, Lmax).ws_bytes;
   return need > 0 ? need : 256;
 }
 
@@ -298,7 +302,7 @@ int tv_tree_verify_attention_paged_fp8(const void* q, const void* k_pool, const 
   if (misaligned(q) || misaligned(out) || misaligned(k_tree) || misaligned(v_tree) ||
       (Lmax > 0 && (misaligned(k_pool) || misaligned(v_pool))))
     return TV_ERR_ALIGN;
-  const tv::AttnPlan p = tv::attn_plan_fp8(B, N, Hq, Hkv, D, Lmax);
+  const tv::AttnPlan p = last_plan<tv::attn_plan_fp8>(B, N, Hq, Hkv, D, Lmax);
   if (p.ws_bytes > 0 && (!workspace || workspace_bytes < p.ws_bytes)) return TV_ERR_WORKSPACE;
   if (misaligned(workspace)) return TV_ERR_ALIGN;
   if (!(scale > 0.f)) scale = 1.0f / sqrtf((float)D);
