@@ -51,7 +51,15 @@ static void check(int B, int N, int Hq, int Hkv, int D, int Lmax) {
   }
 }
 
-int main() {
+int main(int argc, char**) {
+  if (argc > 1) {  // the way that each shape of the input takes: D, arrangement, merge (-1: unsplit)
+    int B, N, Hq, Hkv, D, L;
+    while (scanf("%d %d %d %d %d %d", &B, &N, &Hq, &Hkv, &D, &L) == 6) {
+      const AttnPlan p = attn_plan_fp8(B, N, Hq, Hkv, D, L);
+      printf("%d %d %d\n", D, p.arr, p.S == 1 ? -1 : p.fused);
+    }
+    return 0;
+  }
   const int Bs[] = {1, 2, 3, 7, 16, 64, 65, 256, 1024, 1025, 4096}, Ns[] = {1, 2, 5, 16, 31, 32, 33, 64, 100, 512, 2048};
   const int Ls[] = {0, 32, 96, 1024, 5024, 32768, 131072, 1 << 20, 1 << 26};
   const int heads[][2] = {{1, 1}, {4, 2}, {8, 8}, {32, 4}, {32, 8}, {64, 8}, {24, 8}, {16, 1}, {7, 7}, {40, 10}};

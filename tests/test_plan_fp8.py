@@ -1,6 +1,7 @@
 """Plans of the attention over the 8-bit cache, checked on the host (the plan header is plain C++),
 and the register use of its kernels."""
 import os
+import random
 import re
 import shutil
 import subprocess
@@ -8,6 +9,7 @@ import subprocess
 import pytest
 
 from paper_2606_18394_amd import build
+import test_gpu_fp8_plans
 from test_kernel_registers import READELF, code_objects
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
@@ -29,6 +31,30 @@ def test_plans(tmp_path, flags):
     res = subprocess.run([str(exe)], capture_output=True, text=True)
     assert res.returncode == 0 and "FAIL" not in res.stdout, res.stdout[-2000:] + res.stderr[-1000:]
     assert int(re.search(r"\d+", res.stdout).group()) > 10000
+
+
+@pytest.mark.skipif(shutil.which("g++") is None, reason="needs g++")
+def test_every_way_has_a_case(tmp_path):
+    """All arrangements, unsplit and with either merge, that a draw of shapes takes are among the GPU
+    parity cases."""
+    exe = tmp_path / "plan_fp8_check"
+    subprocess.run(["g++", "-std=c++17", "-O1", "-I", CSRC,
+                    os.path.join(ROOT, "tests", "native", "plan_fp8_check.cpp"), "-o", str(exe)], check=True)
+
+    def ways(shapes):
+        res = subprocess.run([str(exe), "-"], input="".join("%d %d %d %d %d %d\n" % s for s in shapes),
+                             capture_output=True, text=True, check=True)
+        return set(res.stdout.splitlines())
+
+    rng = random.Random(4)
+    drawn = []
+    for _ in range(40000):
+        hq, hkv = rng.choice([(4, 2), (32, 8), (32, 4), (8, 8), (16, 8), (8, 1), (24, 8), (2, 1), (64, 8),
+                              (1, 1), (16, 1)])
+        drawn.append((rng.choice([1, 1, 2, 3, 5, 9, 20, 40]), rng.choice([1, 2, 17, 33, 64, 100, 150, 300, 512]),
+                      hq, hkv, rng.choice([64, 128]), 32 * rng.choice([8, 20, 40, 64, 100, 128, 200, 300, 1000])))
+    taken = ways(drawn)
+    assert len(taken) >= 40 and taken <= ways(test_gpu_fp8_plans.CASES), taken - ways(test_gpu_fp8_plans.CASES)
 
 
 @pytest.mark.skipif(not shutil.which(READELF), reason="needs llvm-readelf")
