@@ -170,8 +170,10 @@ int tv_tree_verify_attention_paged(const void* q, const void* k_pool, const void
  * block table clamping included.  Codes of visible positions must not be NaN
  * (0x7F, 0xFF).  Rows at or behind kv_len are never used, whatever they hold.
  * The workspace is tv_tree_verify_attention_paged_fp8_workspace(B, N, Hq,
- * Hkv, D, max_blocks * block_size) bytes, zero-filled before first use.
+ * Hkv, D, max_blocks * block_size) bytes, of which the first TV_SYNC_BYTES
+ * (or all, if fewer) have to be zeros before first use.
  */
+#define TV_SYNC_BYTES 32768
 size_t tv_tree_verify_attention_paged_fp8_workspace(int B, int N, int Hq, int Hkv, int D, int Lmax);
 int tv_tree_verify_attention_paged_fp8(const void* q, const void* k_pool, const void* v_pool,
                                        const uint8_t* k_exp, const uint8_t* v_exp,
@@ -216,6 +218,12 @@ int tv_commit_path_paged_fp8(const void* k_tree, const void* v_tree, const int32
                              uint8_t* v_exp, const int32_t* block_table, int block_size, int max_blocks,
                              int num_blocks, int32_t* kv_len, int B, int N, int Hkv, int D, int Dmax,
                              hipStream_t stream);
+
+/* A number of the graph capture that `stream` takes part in, different for
+ * every capture of a process; 0 outside any.  (Graphs may be replayed at the
+ * same time, whichever streams they were captured on: what calls of different
+ * captures write as scratch must not be shared.) */
+unsigned long long tv_capture_id(hipStream_t stream);
 
 /* ---- Pages: whose is whose --------------------------------------------
  *

@@ -73,6 +73,8 @@ def load_library() -> ctypes.CDLL:
         lib.tv_tree_verify_attention_paged_fp8.argtypes = (
             [vp] * 5 + [i32p] + [ci] * 3 + [vp, vp, i32p, i32p, vp] + [ci] * 5
             + [ctypes.c_float, vp, sz, vp])
+        lib.tv_capture_id.restype = ctypes.c_ulonglong
+        lib.tv_capture_id.argtypes = [vp]
         lib.tv_append_paged_fp8.restype = ci
         lib.tv_append_paged_fp8.argtypes = [vp] * 8 + [ci] * 3 + [i32p] + [ci] * 4 + [vp]
         lib.tv_commit_path_paged_fp8.restype = ci
@@ -126,7 +128,7 @@ def _connect(lib) -> None:
     except ImportError:
         return
     native.connect(lib._handle, _raw_stream, getattr(torch._C, "_cuda_getDevice", lambda: -1),
-                   workspace)
+                   workspace, _capture_workspace)
     _direct = native
 
 
@@ -305,6 +307,32 @@ def tree_verify_attention_paged(q, k_pool, v_pool, block_table, k_tree, v_tree, 
     return out
 
 
+_SYNC_BYTES = 1 << 15  # of the attention's workspace, which have to start as zeros
+_captures = {}
+
+
+def _capture_workspace(capture: int, nbytes: int, device, stream_ptr: int) -> torch.Tensor:
+    """The attention's workspace of the calls that graph capture `capture` records
+    on a stream.  It lies in the graph's own memory and is cleared by the graph:
+    graphs captured on one stream may be replayed at the same time, and beside
+    eager calls on that stream."""
+    key = (_device_name(device), stream_ptr)
+    last, ws = _captures.get(key, (0, None))
+    if last != capture or ws.numel() < nbytes:
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        if nbytes > _SYNC_BYTES:  # (else the call does not use it)
+            ws[:_SYNC_BYTES].zero_()
+        _captures[key] = capture, ws
+    return ws
+
+
+def _attention_workspace(nbytes: int, device, stream_ptr: int) -> torch.Tensor:
+    capture = load_library().tv_capture_id(stream_ptr)
+    if capture:
+        return _capture_workspace(capture, nbytes, device, stream_ptr)
+    return workspace("attn", nbytes, device, stream_ptr)
+
+
 _BF16, _F8, _U8, _I32 = torch.bfloat16, torch.float8_e4m3fn, torch.uint8, torch.int32
 
 
@@ -349,6 +377,8 @@ def tree_verify_attention_paged_fp8(q, k_pool, v_pool, k_exp, v_exp, block_table
     block_size // 32] uint8; block_table [B, max_blocks] int32; q, k_tree,
     v_tree, out bf16 as in tree_verify_attention (no tree-tail layout);
     parent [B, N] int32, or None for a chain (N = 1: single-token decoding).
+    Without workspace_tensor (zeros before its first use) a stream's calls share
+    one, and the calls of a graph capture have one of their own.
     """
     if _direct is not None:
         done = _direct.attention(q, k_pool, v_pool, k_exp, v_exp, block_table, k_tree, v_tree, parent,
@@ -373,13 +403,17 @@ def tree_verify_attention_paged_fp8(q, k_pool, v_pool, k_exp, v_exp, block_table
     _need_all(dev, index, specs)
     stream = _raw_stream(index)
     need = _bytes("tv_tree_verify_attention_paged_fp8_workspace", B, N, Hq, Hkv, D, mb * bs)
-    ws = workspace_tensor if workspace_tensor is not None else workspace("attn", need, dev, stream)
+    ws = workspace_tensor
+    if ws is None:
+        ws = _attention_workspace(need, dev, stream)
+    else:
+        _need(ws, "workspace_tensor", ws.dtype, device=dev)
     with _current(index):
         rc = lib.tv_tree_verify_attention_paged_fp8(
             q.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(), k_exp.data_ptr(), v_exp.data_ptr(),
             block_table.data_ptr(), bs, mb, nb, k_tree.data_ptr(), v_tree.data_ptr(), pp, lp,
             out.data_ptr(), B, N, Hq, Hkv, D, 0.0 if scale is None else float(scale), ws.data_ptr(),
-            ws.numel(), stream)
+            ws.nbytes, stream)
     if rc:
         _check(rc)
     return out
@@ -573,15 +607,17 @@ def compact_pages(block_table, ref_count, pools=(), n_live=None, copy_src=None, 
     n_live = _output(n_live, "n_live", _I32, (1,), dev)
     copy_src, copy_dst = _outputs((copy_src, copy_dst), ("copy_src", "copy_dst"),
                                   ((nb // 2,),) * 2, dev)
-    stream = _raw_stream(index)
     need = _bytes("tv_compact_pages_workspace", nb)
-    ws = workspace_tensor if workspace_tensor is not None else workspace("pages", need, dev, stream)
+    if workspace_tensor is None:
+        workspace_tensor = torch.empty(need, dtype=_U8, device=dev)
+    _need(workspace_tensor, "workspace_tensor", workspace_tensor.dtype, device=dev)
     # (a single page cannot move, and its empty lists have no address)
     none = n_live.data_ptr()
     with _current(index):
         rc = lib.tv_compact_pages(block_table.data_ptr(), ref_count.data_ptr(), B, mb, nb, base, size,
                                   count, none, copy_src.data_ptr() or none, copy_dst.data_ptr() or none,
-                                  ws.data_ptr(), ws.numel(), stream)
+                                  workspace_tensor.data_ptr(), workspace_tensor.nbytes,
+                                  _raw_stream(index))
     if rc:
         _check(rc)
     return n_live, copy_src, copy_dst

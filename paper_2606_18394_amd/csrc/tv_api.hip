@@ -15,6 +15,7 @@
 
 static_assert(TV_MAX_NODES == tv::kMaxNodes, "node limit mismatch");
 static_assert(TV_MAX_DRAFT_DEPTH == tv::kMaxDraftDepth, "draft depth limit");
+static_assert(TV_SYNC_BYTES == tv::kSyncBytes, "what has to start as zeros");
 static_assert(TV_MAX_POOLS == tv::kMaxPools && TV_MAX_FORKS == tv::kMaxForks &&
               TV_MAX_RESERVE == tv::kMaxReserve, "page call limits");
 
@@ -398,6 +399,16 @@ int tv_commit_path_paged_fp8(const void* k_tree, const void* v_tree, const int32
                                             v_exp, block_table, block_shift(block_size), max_blocks,
                                             num_blocks, kv_len, B, N, Dmax, Hkv, D, stream);
   return e == hipSuccess ? TV_OK : TV_ERR_LAUNCH;
+}
+
+unsigned long long tv_capture_id(hipStream_t stream) {
+  hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+  unsigned long long id = 0;
+  if (hipStreamGetCaptureInfo(stream, &status, &id) != hipSuccess) {
+    (void)hipGetLastError();  // (the null stream while another thread captures)
+    return 0;
+  }
+  return status == hipStreamCaptureStatusActive ? id : 0;
 }
 
 // The page calls' common arguments; block_size 0 where the call has none.

@@ -19,10 +19,12 @@ constexpr int TV_OK = 0, TV_ERR_LAUNCH = -6;  // as in treeverify.h
 constexpr ScalarType kF8 = ScalarType::Float8_e4m3fn, kBF16 = ScalarType::BFloat16,
                      kI32 = ScalarType::Int, kU8 = ScalarType::Byte;
 
-// binding.py's: the current stream of a device, the current device, a workspace
-PyObject *raw_stream, *current_device, *workspace;
+// binding.py's: the current stream of a device, the current device, a stream's workspace
+// for the attention, a capture's
+PyObject *raw_stream, *current_device, *workspace, *capture_workspace;
 
 struct Library {
+  unsigned long long (*capture_id)(void*);
   size_t (*attention_ws)(int, int, int, int, int, int);
   int (*attention)(const void*, const void*, const void*, const void*, const void*, const void*, int, int,
                    int, const void*, const void*, const void*, const void*, void*, int, int, int, int, int,
@@ -169,19 +171,22 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     PyObject* ws = a[12];
     PyObject* own = nullptr;
     if (ws == Py_None) {
-      PyObject* args[4] = {PyUnicode_FromString("attn"), PyLong_FromSize_t(need),
-                           PyObject_GetAttrString(a[0], "device"), PyLong_FromVoidPtr(stream)};
-      ws = own = PyObject_Vectorcall(workspace, args, 4, nullptr);
+      const unsigned long long capture = lib.capture_id(stream);
+      PyObject* args[4] = {capture ? PyLong_FromUnsignedLongLong(capture) : PyUnicode_FromString("attn"),
+                           PyLong_FromSize_t(need), PyObject_GetAttrString(a[0], "device"),
+                           PyLong_FromVoidPtr(stream)};
+      ws = own = PyObject_Vectorcall(capture ? capture_workspace : workspace, args, 4, nullptr);
       for (PyObject* o : args) Py_XDECREF(o);
     }
-    if (!ws || !THPVariable_Check(ws)) {
+    if (!ws || !t.any(ws)) {
       Py_XDECREF(own);
       return none();
     }
     const at::Tensor& w = THPVariable_Unpack(ws);
+    const size_t bytes = (size_t)w.nbytes();
     const int rc = lib.attention(q->data_ptr(), c.k, c.v, c.ke, c.ve, c.table, (int)c.bs, (int)c.mb,
                                  (int)c.nb, ktp, vtp, parent, len, out, (int)B, (int)N, (int)Hq, (int)Hkv,
-                                 (int)D, (float)scale, w.data_ptr(), (size_t)w.numel(), stream);
+                                 (int)D, (float)scale, w.data_ptr(), bytes, stream);
     Py_XDECREF(own);
     return done(rc, a[9]);
   });
@@ -311,10 +316,10 @@ PyObject* free_pages(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// handle of the loaded library, raw_stream, current_device, workspace
+// handle of the loaded library, raw_stream, current_device, workspace, capture_workspace
 PyObject* connect(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  if (n != 4) {
-    PyErr_SetString(PyExc_TypeError, "connect(handle, raw_stream, current_device, workspace)");
+  if (n != 5) {
+    PyErr_SetString(PyExc_TypeError, "connect takes five arguments");
     return nullptr;
   }
   void* handle = PyLong_AsVoidPtr(a[0]);
@@ -323,15 +328,16 @@ PyObject* connect(PyObject*, PyObject* const* a, Py_ssize_t n) {
     f = reinterpret_cast<std::remove_reference_t<decltype(f)>>(dlsym(handle, name));
     return f != nullptr;
   };
-  if (!find(lib.attention_ws, "tv_tree_verify_attention_paged_fp8_workspace") ||
+  if (!find(lib.capture_id, "tv_capture_id") ||
+      !find(lib.attention_ws, "tv_tree_verify_attention_paged_fp8_workspace") ||
       !find(lib.attention, "tv_tree_verify_attention_paged_fp8") || !find(lib.append, "tv_append_paged_fp8") ||
       !find(lib.commit, "tv_commit_path_paged_fp8") || !find(lib.reserve, "tv_reserve_pages") ||
       !find(lib.fork, "tv_fork_pages") || !find(lib.free_, "tv_free_pages")) {
     PyErr_SetString(PyExc_RuntimeError, "libtreeverify.so lacks an entry point");
     return nullptr;
   }
-  PyObject** kept[3] = {&raw_stream, &current_device, &workspace};
-  for (int k = 0; k < 3; ++k) {
+  PyObject** kept[4] = {&raw_stream, &current_device, &workspace, &capture_workspace};
+  for (int k = 0; k < 4; ++k) {
     Py_INCREF(a[k + 1]);
     Py_XDECREF(*kept[k]);
     *kept[k] = a[k + 1];

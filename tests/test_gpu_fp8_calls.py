@@ -240,6 +240,53 @@ def test_two_streams_at_once():
         assert np.array_equal(bits(args[9]), w)
 
 
+def test_graphs_of_one_stream_at_once(monkeypatch):
+    """Graphs captured on one stream, replayed on two streams at the same time and beside eager
+    calls: each has a workspace of its own, cleared by itself, and its calls share it."""
+    jobs = [attention_args(c) for c in (4, 10)]
+    want = []
+    for args, kv in jobs:
+        tv.tree_verify_attention_paged_fp8(*args, kv_len=kv)
+        want.append(bits(args[9]))
+    lib = binding.load_library()
+    sizes = [(*a[0].shape[:3], a[6].shape[2], a[0].shape[3], a[5].shape[1] * a[1].shape[2]) for a, _ in jobs]
+    assert all(lib.tv_tree_verify_attention_paged_fp8_workspace(*s) > 1 << 15 for s in sizes)  # both split
+    given = []
+    real = binding._capture_workspace
+    assert lib.tv_capture_id(torch.cuda.current_stream().cuda_stream) == 0
+    monkeypatch.setattr(binding, "_direct", None)
+    monkeypatch.setattr(binding, "_capture_workspace", lambda *a: given.append((a[0], real(*a))) or given[-1][1])
+    side = torch.cuda.Stream()
+    graphs, outs = [], []
+    torch.cuda.synchronize()
+    for args, kv in jobs:
+        graph = torch.cuda.CUDAGraph()
+        outs.append([torch.empty_like(args[9]) for _ in range(3)])
+        with torch.cuda.graph(graph, stream=side):
+            for out in outs[-1]:
+                tv.tree_verify_attention_paged_fp8(*args[:9], out, kv_len=kv)
+        graphs.append(graph)
+    ids, at = [g[0] for g in given], [g[1].data_ptr() for g in given]
+    assert len(ids) == 6 and len(set(ids[:3])) == len(set(ids[3:])) == 1 and ids[0] != ids[3]
+    assert len(set(at[:3])) == len(set(at[3:])) == 1 and at[0] != at[3]
+    streams = [torch.cuda.Stream() for _ in jobs]
+    for turn in range(4):
+        for o in outs[0] + outs[1]:
+            o.zero_()
+        torch.cuda.synchronize()
+        for _ in range(6):
+            for s, g in zip(streams, graphs):
+                with torch.cuda.stream(s):
+                    g.replay()
+            with torch.cuda.stream(side):
+                for args, kv in jobs:
+                    tv.tree_verify_attention_paged_fp8(*args, kv_len=kv)
+        torch.cuda.synchronize()
+        for (args, _), o, w in zip(jobs, outs, want):
+            for got in o + [args[9]]:
+                assert np.array_equal(bits(got), w)
+
+
 def test_far_pages():
     """Offsets beyond 32 bits: a pool of more than 4 GiB, whose last pages are the ones in use."""
     Hkv, D, bs = 8, 128, 1024
