@@ -168,7 +168,8 @@ int tv_tree_verify_attention_paged(const void* q, const void* k_pool, const void
  * single-token decoding.  Codes enter the products as the exact bf16 values
  * they stand for; everything else is as in tv_tree_verify_attention_paged,
  * block table clamping included.  Codes of visible positions must not be NaN
- * (0x7F, 0xFF).  Rows at or behind kv_len are never used, whatever they hold.
+ * (0x7F, 0xFF), and all N tree nodes' keys and values, a padded tree's too, are
+ * finite.  Rows at or behind kv_len are never used, whatever they hold.
  * The workspace is tv_tree_verify_attention_paged_fp8_workspace(B, N, Hq,
  * Hkv, D, max_blocks * block_size) bytes, of which the first TV_SYNC_BYTES
  * (or all, if fewer) have to be zeros before first use.
@@ -198,11 +199,12 @@ int tv_tree_verify_attention_paged_fp8(const void* q, const void* k_pool, const 
  * new codes are the nearest to x * 2^(127 - e) (ties to even), and older
  * codes the nearest to what they stand for (so unchanged unless the byte
  * grew).  Positions behind the last row keep what they hold.  A sequence
- * whose n_new is outside [0, T], whose kv_len is negative, or that would pass
- * its max_blocks pages is left unchanged (pools, exponents and kv_len).
- * Entries of block_table are clamped into the pool.  The pages that a
- * sequence writes to must be its own: not shared with another one, which a
- * partly filled page after tv_fork_pages is not.
+ * whose n_new is outside [0, T], whose kv_len is negative, or that lacks a
+ * page for one of its rows (it would pass its max_blocks pages, or an entry of
+ * its block_table is outside [0, num_blocks)) is left unchanged: pools,
+ * exponents and kv_len.  The pages that a sequence writes to must be its own:
+ * not shared with another one, which a partly filled page after tv_fork_pages
+ * is not.
  */
 int tv_append_paged_fp8(const void* k_new, const void* v_new, const int32_t* n_new, void* k_pool,
                         void* v_pool, uint8_t* k_exp, uint8_t* v_exp, const int32_t* block_table,
@@ -212,7 +214,8 @@ int tv_append_paged_fp8(const void* k_new, const void* v_new, const int32_t* n_n
 /* tv_commit_path into the 8-bit cache: the rows path[b, 0 .. accept_len[b] - 1]
  * of k_tree, v_tree [B, N, Hkv, D] bf16 are appended as by
  * tv_append_paged_fp8; sequences are left unchanged where tv_commit_path
- * leaves them (failed or too long acceptance, a node outside [0, N), no room). */
+ * leaves them (failed or too long acceptance, a node outside [0, N), no room)
+ * and where pages are lacking. */
 int tv_commit_path_paged_fp8(const void* k_tree, const void* v_tree, const int32_t* path,
                              const int32_t* accept_len, void* k_pool, void* v_pool, uint8_t* k_exp,
                              uint8_t* v_exp, const int32_t* block_table, int block_size, int max_blocks,

@@ -68,13 +68,15 @@ def exponent(a):
 
 def append(pool, exps, table, kv_len, new, n_new):
     """new [B, T, Hkv, D]: row j < n_new[b] goes to position kv_len[b] + j of sequence b.  A
-    sequence whose n_new is outside [0, T] or that would pass its pages is left as it is.
+    sequence whose n_new is outside [0, T] or that lacks a page for one of its rows is left as it is.
     Returns new copies (pool, exps)."""
     pool, exps = np.array(pool, copy=True), np.array(exps, copy=True)
     bs = pool.shape[2]
     for b in range(len(kv_len)):
         kv, n = int(kv_len[b]), int(n_new[b])
         if not 0 <= n <= new.shape[1] or kv < 0 or kv + n > table.shape[1] * bs:
+            continue
+        if not all(0 <= p < len(pool) for p in table[b, kv // bs:-(-(kv + n) // bs)]):
             continue
         for lo in range(kv // GROUP * GROUP, kv + n, GROUP):
             if n == 0:
@@ -97,7 +99,7 @@ def append(pool, exps, table, kv_len, new, n_new):
 def commit(pool, exps, table, kv_len, tree, path, accept_len):
     """The accepted path's rows of tree [B, N, Hkv, D] are appended.  A sequence that failed
     acceptance (accept_len < 1), has accept_len above the path's width, names a node outside the
-    tree or would pass its pages is left as it is."""
+    tree or lacks a page is left as it is."""
     B, N = tree.shape[:2]
     path, n = np.asarray(path), np.array(accept_len, np.int64)
     for b in range(B):

@@ -424,7 +424,7 @@ def append_paged_fp8(k_new, v_new, k_pool, v_pool, k_exp, v_exp, block_table, kv
     tree_verify_attention_paged_fp8) behind kv_len, and advance kv_len, in
     place: rows 0 .. n_new[b] - 1 (n_new None: all) of k_new/v_new
     [B,T,Hkv,D] bf16 become codes and exponents.  kv_len, n_new [B] int32.  A
-    sequence without room for its rows is left unchanged."""
+    sequence without pages for all its rows is left unchanged."""
     if _direct is not None and _direct.append(k_new, v_new, k_pool, v_pool, k_exp, v_exp,
                                               block_table, kv_len, n_new):
         return

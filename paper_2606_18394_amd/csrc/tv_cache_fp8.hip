@@ -42,20 +42,34 @@ typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
-// Rows that sequence b gets, 0 where it is left as it is.
-__device__ __forceinline__ int rows_of(const WriteArgs& a, int b, int kv) {
-  const int n = a.n_new ? a.n_new[b] : a.P;
+// What sequence b gets: n rows, 0 where it is left as it is; but that it has a page for
+// all of them is known only once `lacking` is looked at, in any lane.
+struct Rows {
+  int n, page;   // page: of this lane's, the sequence's entry `lane` behind the first one's
+  bool lacking;
+};
+__device__ __forceinline__ Rows rows_of(const WriteArgs& a, int b, int kv) {
+  Rows r{0, -1, false};
+  const int n = a.n_new ? a.n_new[b] : a.P, lane = threadIdx.x & 63;
   const int cap = a.max_blocks << a.shift;
-  if (n < 1 || n > a.P || kv < 0 || kv > cap - n) return 0;
+  if (n < 1 || n > a.P || kv < 0 || kv > cap - n) return r;
+  const int first = kv >> a.shift, last = (kv + n - 1) >> a.shift;
+  const int32_t* row = a.block_table + (size_t)b * a.max_blocks;
+  if (first + lane <= last) {
+    r.page = row[first + lane];
+    r.lacking = r.page < 0 || r.page >= a.num_blocks;
+  }
+  for (int j = first + lane + 64; j <= last; j += 64) r.lacking |= row[j] < 0 || row[j] >= a.num_blocks;
   if (a.path) {
     bool bad = false;
-    for (int j = threadIdx.x & 63; j < n; j += 64) {
+    for (int j = lane; j < n; j += 64) {
       const int node = a.path[(size_t)b * a.P + j];
       bad |= node < 0 || node >= a.T;
     }
-    if (__any(bad)) return 0;
+    if (__any(bad)) return r;
   }
-  return n;
+  r.n = n;
+  return r;
 }
 
 __device__ __forceinline__ float power_of_two(int e) { return __int_as_float((e + 127) << 23); }
@@ -74,20 +88,15 @@ __device__ __forceinline__ int rescaled(int w, float scale) {
   return __builtin_amdgcn_cvt_pk_fp8_f32(hi[0] * scale, hi[1] * scale, half, true);
 }
 
-// Unit (group number g0 + gi, head h, K or V) of sequence b with its n new rows from kv on.
+// Unit (group gi of those that get rows, head h, K or V) of sequence b with its new rows
+// from kv on.
 template <int D>
-__device__ __forceinline__ void write_unit(const WriteArgs& a, int b, int kv, int n, int gi, int h, int isv) {
+__device__ __forceinline__ void write_unit(const WriteArgs& a, int b, int kv, const Rows& rows, int gi, int h,
+                                           int isv) {
   constexpr int kLanes = D / 8, kRows = 64 / kLanes, kLoads = kGroup / kRows;
   const int lane = threadIdx.x & 63, l = lane % kLanes;
-  const int first = ((kv >> 5) + gi) * kGroup;  // the group's first position
+  const int first = ((kv >> 5) + gi) * kGroup, n = rows.n;  // the group's first position
   if (first >= kv + n) return;
-  int blk = a.block_table[(size_t)b * a.max_blocks + (first >> a.shift)];
-  blk = blk < 0 ? 0 : (blk >= a.num_blocks ? a.num_blocks - 1 : blk);
-  const int per = a.shift - 5;
-  const size_t group = (((size_t)blk * a.Hkv + h) << per) + ((first >> 5) & ((1 << per) - 1));
-  const bool older = first < kv;
-  const int was = older ? a.exps[isv][group] : 0;
-
   i32x4 v[kLoads];
   u16x2 most = {0, 0};
 #pragma unroll
@@ -99,6 +108,15 @@ __device__ __forceinline__ void write_unit(const WriteArgs& a, int b, int kv, in
       v[k] = *(const i32x4*)(a.x[isv] + (((size_t)b * a.T + row) * a.Hkv + h) * D + 8 * l);
     }
   }
+  // the rows are on their way: is there a page for each, and which is this group's
+  if (__any(rows.lacking)) return;
+  const int at = (first >> a.shift) - (kv >> a.shift);
+  const int blk = at < 64 ? __builtin_amdgcn_readlane(rows.page, at)
+                          : a.block_table[(size_t)b * a.max_blocks + (first >> a.shift)];
+  const int per = a.shift - 5;
+  const size_t group = (((size_t)blk * a.Hkv + h) << per) + ((first >> 5) & ((1 << per) - 1));
+  const bool older = first < kv;
+  const int was = older ? a.exps[isv][group] : 0;
 #pragma unroll
   for (int k = 0; k < kLoads; ++k)
 #pragma unroll
@@ -137,14 +155,15 @@ __global__ __launch_bounds__(1024) void write_sequence(WriteArgs a) {
   const int b = blockIdx.x, waves = blockDim.x / 64;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int kv = a.kv_len[b];
-  const int n = rows_of(a, b, kv);
-  const int units = n > 0 ? a.groups * 2 * a.Hkv : 0;
+  const Rows rows = rows_of(a, b, kv);
+  const int units = rows.n > 0 ? a.groups * 2 * a.Hkv : 0;
   for (int u = wave; u < units; u += waves) {
     const int h = u % a.Hkv, r = u / a.Hkv;
-    write_unit<D>(a, b, kv, n, r >> 1, h, r & 1);
+    write_unit<D>(a, b, kv, rows, r >> 1, h, r & 1);
   }
+  const bool lacking = __any(rows.lacking);
   __syncthreads();  // every wave has read kv_len
-  if (threadIdx.x == 0 && n > 0) a.kv_len[b] = kv + n;
+  if (threadIdx.x == 0 && rows.n > 0 && !lacking) a.kv_len[b] = kv + rows.n;
 }
 
 // Many: a wave per unit, and kv_len grows in a second kernel.
@@ -158,14 +177,15 @@ __global__ __launch_bounds__(256) void write_groups(WriteArgs a) {
   const long long b = r / a.groups;
   if (b >= a.B) return;
   const int kv = a.kv_len[b];
-  const int n = rows_of(a, (int)b, kv);
-  if (n > 0) write_unit<D>(a, (int)b, kv, n, gi, h, isv);
+  const Rows rows = rows_of(a, (int)b, kv);
+  if (rows.n > 0) write_unit<D>(a, (int)b, kv, rows, gi, h, isv);
 }
 
 __global__ __launch_bounds__(64) void grow_lengths(WriteArgs a) {
   const int b = blockIdx.x, kv = a.kv_len[b];
-  const int n = rows_of(a, b, kv);
-  if (threadIdx.x == 0 && n > 0) a.kv_len[b] = kv + n;
+  const Rows rows = rows_of(a, b, kv);
+  const bool lacking = __any(rows.lacking);
+  if (threadIdx.x == 0 && rows.n > 0 && !lacking) a.kv_len[b] = kv + rows.n;
 }
 
 // x: K's and V's rows [B, T, Hkv, D]; P: rows at most that a sequence gets.

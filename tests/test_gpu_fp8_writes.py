@@ -138,3 +138,48 @@ def test_commit(case):
               for i in range(2)]
     grown = np.where((np.arange(B) >= 1) & (np.arange(B) <= 5) & (B > 5), 0, n)
     check(codes, exps, bt, kvl, expect, kvl + grown, dev)
+
+
+@pytest.mark.parametrize("T,Hkv", [(3, 2), (300, 8)])
+def test_lacking_pages(T, Hkv):
+    """A sequence that has no page for one of its rows is left as it is: entries that were never
+    filled, numbers outside the pool, the last of many pages; the others get their rows."""
+    rng = np.random.default_rng(T)
+    B, D, bs, mb = 6, 64, 32, 100
+    bt, nb = synth.block_table(rng, B, mb)
+    kvl = np.array([0, 40, 31, 32 * 70 + 5, 64, 17], np.int32)
+    bt[0, 0] = -1
+    bt[1, (40 + T - 1) // bs] = nb
+    bt[2, 10 if T == 3 else 5] = -7          # short: behind its rows, so nothing is lacking
+    bt[4, 2 + (T - 1) // bs] = -1
+    kvl[3] = mb * bs - T
+    codes, exps = pools(rng, nb, Hkv, bs, D)
+    new = [values(rng, (B, T, Hkv, D)) for _ in range(2)]
+    rows = np.full(B, T)
+    gets = np.array([0, 0, T == 3, 1, 0, 1])
+    expect = [kv_fp8.append(codes[i], exps[i], bt, kvl, oracle.decode_bf16(new[i]), rows * gets) for i in range(2)]
+    same = kv_fp8.append(codes[0], exps[0], bt, kvl, oracle.decode_bf16(new[0]), rows)
+    assert all(np.array_equal(x, y) for x, y in zip(same, expect[0]))
+    dev = [dev_f8(codes[0]), dev_f8(codes[1]), dev_u8(exps[0]), dev_u8(exps[1]), dev_i32(kvl)]
+    append_paged_fp8(dev_bf16(new[0]), dev_bf16(new[1]), *dev[:4], dev_i32(bt), dev[4])
+    check(codes, exps, bt, kvl, expect, kvl + T * gets, dev)
+    path = np.tile(np.arange(T), (B, 1))
+    dev = [dev_f8(codes[0]), dev_f8(codes[1]), dev_u8(exps[0]), dev_u8(exps[1]), dev_i32(kvl)]
+    commit_path_paged_fp8(dev_bf16(new[0]), dev_bf16(new[1]), dev_i32(path), dev_i32(rows), *dev[:4],
+                          dev_i32(bt), dev[4])
+    check(codes, exps, bt, kvl, expect, kvl + T * gets, dev)
+
+
+def test_many_pages_are_all_looked_at():
+    """More than 64 pages for one sequence's rows, and the last of them is missing."""
+    rng = np.random.default_rng(9)
+    B, T, Hkv, D, bs, mb = 2, 2900, 1, 64, 32, 100
+    bt, nb = synth.block_table(rng, B, mb)
+    kvl = np.array([100, 100], np.int32)
+    bt[1, (100 + T - 1) // bs] = -1
+    codes, exps = pools(rng, nb, Hkv, bs, D)
+    new = [values(rng, (B, T, Hkv, D)) for _ in range(2)]
+    dev = [dev_f8(codes[0]), dev_f8(codes[1]), dev_u8(exps[0]), dev_u8(exps[1]), dev_i32(kvl)]
+    append_paged_fp8(dev_bf16(new[0]), dev_bf16(new[1]), *dev[:4], dev_i32(bt), dev[4])
+    expect = [kv_fp8.append(codes[i], exps[i], bt, kvl, oracle.decode_bf16(new[i]), [T, 0]) for i in range(2)]
+    check(codes, exps, bt, kvl, expect, kvl + np.array([T, 0]), dev)
