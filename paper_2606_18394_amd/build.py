@@ -5,6 +5,8 @@ import os
 import shutil
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -35,18 +37,28 @@ def hipcc() -> str:
 
 
 def build(verbose: bool = False) -> str:
-    """Compile every source into LIB (always rebuilds).  Returns the path."""
+    """Compile every source into LIB (always rebuilds), four at a time.  Returns the path."""
     tmp = LIB + ".tmp"
-    cmd = [hipcc()] + HIPCC_FLAGS + [os.path.join(CSRC, s) for s in SOURCES] + ["-o", tmp]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    msgs = "\n".join(l for l in (res.stdout + res.stderr).splitlines()
-                     if "packed-fp32-ops" not in l)
-    if res.returncode != 0:
-        raise RuntimeError("hipcc failed:\n" + msgs)
-    if verbose and msgs.strip():
-        print(msgs)
+    flags = [f for f in HIPCC_FLAGS if f != "-shared"]
+
+    def run(cmd):
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        res = subprocess.run(cmd, capture_output=True, text=True)
+        msgs = "\n".join(l for l in (res.stdout + res.stderr).splitlines()
+                         if "packed-fp32-ops" not in l)
+        if res.returncode != 0:
+            raise RuntimeError("hipcc failed:\n" + msgs)
+        if verbose and msgs.strip():
+            print(msgs)
+
+    with tempfile.TemporaryDirectory() as objs, ThreadPoolExecutor(4) as jobs:
+        out = [os.path.join(objs, s + ".o") for s in SOURCES]
+        # (the longest first)
+        order = sorted(zip(SOURCES, out), key=lambda so: -os.path.getsize(os.path.join(CSRC, so[0])))
+        list(jobs.map(lambda so: run([hipcc()] + flags + ["-c", os.path.join(CSRC, so[0]), "-o", so[1]]),
+                      order))
+        run([hipcc()] + HIPCC_FLAGS + out + ["-o", tmp])
     os.replace(tmp, LIB)
     return LIB
 
