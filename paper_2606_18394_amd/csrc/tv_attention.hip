@@ -802,25 +802,6 @@ __global__ __launch_bounds__(256) void attn_combine(AttnArgs a) {
              bad != 0);
 }
 
-template <int D, int RB>
-static hipError_t launch_combine_t(const AttnArgs& a, hipStream_t st) {
-  const int frags = a.B * a.Hkv * a.nRB * (D / 16) * (RB / 16);
-  hipLaunchKernelGGL((attn_combine<D, RB>), dim3(frags / 4), dim3(256), 0, st, a);
-  return hipGetLastError();
-}
-
-// The second kernel for the other cache kind's main kernels (row blocks of 16 to 256).
-hipError_t launch_combine(const AttnArgs& a, int D, int RB, hipStream_t st) {
-  switch (RB) {
-    case 16: return D == 128 ? launch_combine_t<128, 16>(a, st) : launch_combine_t<64, 16>(a, st);
-    case 32: return D == 128 ? launch_combine_t<128, 32>(a, st) : launch_combine_t<64, 32>(a, st);
-    case 64: return D == 128 ? launch_combine_t<128, 64>(a, st) : launch_combine_t<64, 64>(a, st);
-    case 128: return D == 128 ? launch_combine_t<128, 128>(a, st) : launch_combine_t<64, 128>(a, st);
-    case 256: return D == 128 ? launch_combine_t<128, 256>(a, st) : launch_combine_t<64, 256>(a, st);
-    default: return hipErrorInvalidValue;
-  }
-}
-
 template <int D, int WR, int WK, int NS, bool kPaged, bool kShareQ>
 static hipError_t launch_main(const AttnArgs& a, const AttnPlan& p, hipStream_t st) {
   // the kernel's LDS limit on each device, raised only when a call needs more
@@ -862,7 +843,10 @@ static hipError_t launch_attn_t(const AttnArgs& a, const AttnPlan& p, hipStream_
     else
       e = launch_main<D, ar.WR, ar.WK, NS, kPaged, false>(a, p, st);
     if (e != hipSuccess || p.S == 1 || p.fused) return e;
-    return launch_combine_t<D, kRowsPerWave * ar.WR>(a, st);
+    constexpr int RB = kRowsPerWave * ar.WR;
+    const int frags = a.B * a.Hkv * p.nRB * (D / 16) * (RB / 16);
+    hipLaunchKernelGGL((attn_combine<D, RB>), dim3(frags / 4), dim3(256), 0, st, a);
+    return hipGetLastError();
   }
 }
 

@@ -5,7 +5,7 @@
 // exponent byte e per group of 32 positions, page and head: a code stands for
 // code * 2^(e - 127).  The tree's own K and V are bf16.  Its work decomposition is that
 // of tv_attention.hip too: 32-key tiles in chunks of one size for the whole batch, a
-// workgroup per chunk and block of 32 * WR rows, WR x WK waves, an LDS ring per key
+// workgroup per chunk and block of 16 * NT * WR rows, WR x WK waves, an LDS ring per key
 // group, chunk partials merged by the last workgroup or by a second kernel.
 //
 // Layout.  A page holds its heads one after the other, [num_blocks, Hkv, block_size, D],
@@ -658,7 +658,100 @@ void attn_fp8(Fp8Args a) {
   if (wave < kMerge) merge_chunks<D, RB, kMerge>(z, part0, nval, b, g, r0, bad, wave, lane);
 }
 
-hipError_t launch_combine(const AttnArgs& a, int D, int RB, hipStream_t st);  // tv_attention.hip
+// Second kernel of the plans whose merge is too much for one workgroup:
+// out = sum_s e_s O_s / sum_s e_s l_s with e_s = 2^(m_s - m*).  A workgroup per 16 x 16
+// fragment, whose four waves take the row block's chunks in turn and are joined in LDS
+// (two trees of 16 nodes over 131072 rows, 64 chunks each: 114.4 us, with a wave per
+// fragment 119.7).
+// What can be asked for before the number of chunks is known is asked for at once, as in
+// attn_combine (slots past the chunks lie inside the workspace).
+template <int D, int RB>
+__global__ __launch_bounds__(256) void combine_fp8(Fp8Args a) {
+  constexpr int NTG = RB / 16, DT = D / 16, U = 8, W = 4;
+  constexpr int kParPerThread = kMaxNodes / 256;
+  __shared__ f32x4 accs[W][64];
+  __shared__ float2 mls[W][16];
+  const int lane = threadIdx.x & 63, l16 = lane & 15, g4 = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int f = blockIdx.x % (DT * NTG), blk = blockIdx.x / (DT * NTG);
+  const int rb = blk % a.nRB, g = blk / a.nRB % a.Hkv, b = blk / a.nRB / a.Hkv;
+  const int dt = f / NTG, ntg = f % NTG;
+  const int row = ntg * 16 + l16, r = rb * RB + row;
+  if (rb * RB + ntg * 16 >= a.M) return;  // no rows: nothing was stored
+  int pv[kParPerThread];
+#pragma unroll
+  for (int k = 0; k < kParPerThread; ++k) {
+    const int i = threadIdx.x + 256 * k;
+    pv[k] = i >= a.N ? 0 : (a.parent ? a.parent[(size_t)b * a.N + i] : i - 1);
+  }
+  const int i_hi = (min(rb * RB + RB, a.M) - 1) / a.G;
+  EvenItem ev{a.chunk, b, 0, 0, 0};
+  if (a.B > 1) ev = even_split<false>(a, -1, b, 0);
+  const size_t base = (size_t)(g * a.nRB + rb) * a.slots + ev.first;  // the first chunk partial
+  const int nslot = a.slots - ev.first;
+  float2 ml[U];
+  f32x4 ov[U];
+  auto ask = [&](int s0, int end) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int s = s0 + W * u;
+      if (s < end) {
+        ml[u] = a.ws_ml[(base + s) * RB + row];
+        ov[u] = a.ws_o[((base + s) * DT * NTG + dt * NTG + ntg) * 64 + lane];
+      }
+    }
+  };
+  ask(wave, nslot);
+  if (a.B == 1) ev = even_one<false>(a, 0, 0);
+  const int nval = (segment(a, ev.kvl, i_hi).T + ev.chunk - 1) / ev.chunk;
+  if (nval == 1) return;  // written by its only chunk
+  float m = -INFINITY, l = 0.f;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  for (int s0 = wave; s0 < nval; s0 += W * U) {
+    if (s0 >= W * U) ask(s0, nval);
+    float mb = m;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (s0 + W * u < nval) mb = fmaxf(mb, ml[u].x);
+    if (mb != -INFINITY) {  // else every chunk so far saw no key: nothing to add
+      const float ea = __builtin_amdgcn_exp2f(m - mb);  // 0 while m = -inf
+      l *= ea;
+      acc *= ea;
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (s0 + W * u < nval && ml[u].x != -INFINITY) {
+          const float e = __builtin_amdgcn_exp2f(ml[u].x - mb);
+          l += e * ml[u].y;
+          acc += e * ov[u];
+        }
+      m = mb;
+    }
+  }
+  int bad = 0;
+#pragma unroll
+  for (int k = 0; k < kParPerThread; ++k) {
+    const int i = threadIdx.x + 256 * k;
+    if (i < a.N) bad |= (i == 0) ? (pv[k] != -1) : (pv[k] < 0 || pv[k] >= i);
+  }
+  accs[wave][lane] = acc;
+  if (g4 == 0) mls[wave][l16] = make_float2(m, l);
+  bad = __syncthreads_or(bad);
+  if (wave > 0 || r >= a.M) return;
+  float mstar = -INFINITY;
+#pragma unroll
+  for (int w = 0; w < W; ++w) mstar = fmaxf(mstar, mls[w][l16].x);
+  l = 0.f;
+  acc = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int w = 0; w < W; ++w) {
+    const float mw = mls[w][l16].x;
+    const float e = mw == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mw - mstar);
+    l += e * mls[w][l16].y;
+    acc += e * accs[w][lane];
+  }
+  const int node = r / a.G, h = g * a.G + r % a.G;
+  store_out4(a.out + ((size_t)(b * a.N + node) * a.Hq + h) * D + 16 * dt + 4 * g4, acc, 1.f / l, bad != 0);
+}
 
 template <int D, int ARR>
 static hipError_t launch_fp8_t(const Fp8Args& a, const AttnPlan& p, hipStream_t st) {
@@ -685,7 +778,10 @@ static hipError_t launch_fp8_t(const Fp8Args& a, const AttnPlan& p, hipStream_t 
                      a);
   e = hipGetLastError();
   if (e != hipSuccess || p.S == 1 || p.fused) return e;
-  return launch_combine(a, D, p.RB, st);
+  constexpr int RB = 16 * ar.NT * ar.WR;
+  const int frags = a.B * a.Hkv * a.nRB * (D / 16) * (RB / 16);
+  hipLaunchKernelGGL((combine_fp8<D, RB>), dim3(frags), dim3(256), 0, st, a);
+  return hipGetLastError();
 }
 
 template <int D, int K = 0>

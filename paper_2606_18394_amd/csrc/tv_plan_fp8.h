@@ -73,9 +73,10 @@ inline bool attn_plan_fp8_fits(const AttnPlan& p) {
 // CU's share of 8 waves at work); then the fixed costs, HBM (also what the CUs at work
 // can ask for), the tree and the partials.  The constants are fitted together to 294
 // shapes drawn over the ranges of 1 to 64 sequences, 1 to 512 nodes, up to 131072 rows
-// and the heads above, each in all arrangements and up to 14 splits and merges: the plan
-// picked is 2.0% slower than the fastest on average, also on 120 shapes that the fit has
-// not seen (row blocks as large as the tree fills, split to fill the GPU once: 18%).
+// and the heads above, each in all arrangements and up to 14 splits and merges, those of
+// the merge by a second kernel to 6000 times of both merges.  The plan picked is 2.1%
+// slower than the fastest on average on 1400 shapes that the fit has not seen (row blocks
+// as large as the tree fills, split to fill the GPU once: 18%).
 constexpr double kFp8Fill = 0.703;  // mean length of several sequences over the capacity
 constexpr double kFp8Full[] = {1.04, 0, 1.598, 1.582, 1.414, 1.202, 0.911};  // 8 waves at work
 static_assert(sizeof(kFp8Full) / sizeof(kFp8Full[0]) == kNumArrangementsFp8, "one per arrangement");
@@ -125,7 +126,8 @@ inline double attn_plan_fp8_cost(AttnPlan& p, int B, int Hkv, int D, int Lmax, i
     const int active = waves_wg >= NTG ? waves_wg / NTG * rows : (rows < waves_wg ? rows : waves_wg);
     const double block = rows * 16.0 * D * 4.0, all = wgs / p.nRB * cdiv(p.M, 16) * 16.0 * D * 4.0;
     const double fused = 2.63 + chunks * block / (active * 15.4e3 < 86.7e3 ? active * 15.4e3 : 86.7e3);
-    const double second = 5.46 + all / 2.71e6;
+    const double frags = (double)B * Hkv * cdiv(p.M, 16) * (D / 16);
+    const double second = 2.87 + all / 2.49e6 + 0.00306 * frags;
     p.fused = fused <= second;
     t += (p.fused ? fused : second) + all / 5.0e6;
   }

@@ -51,6 +51,11 @@ CASES = [
     (40, 33, 16, 8, 128, 256),
     (3, 100, 8, 1, 128, 16000),
     (20, 33, 24, 8, 128, 2048),
+    (20, 1, 1, 1, 128, 2048),
+    (2, 1, 8, 8, 128, 1280),
+    (9, 1, 1, 1, 64, 6400),
+    (5, 1, 1, 1, 64, 2048),
+    (9, 100, 2, 1, 64, 3200),
 ]
 
 

@@ -72,7 +72,7 @@ def test_kernels_do_not_spill(tmp_path):
                                check=True).stdout
         for entry in re.split(r"\n\s*- \.agpr_count:", notes)[1:]:
             name = re.search(r"\n\s*\.name:\s*(\S+)", entry).group(1)
-            if not re.search(r"attn_fp8|write_|grow_|reserve_|fork_|free_|copy_|compact_", name):
+            if not re.search(r"(attn|combine)_fp8|write_|grow_|reserve_|fork_|free_|copy_|compact_", name):
                 continue
             seen[name] = [int(re.search(rf"\n\s*\.{f}:\s*(\d+)\n", entry).group(1))
                           for f in ("vgpr_spill_count", "private_segment_fixed_size")]
