@@ -26,6 +26,7 @@
 
 #include <atomic>
 #include <mutex>
+#include <type_traits>
 
 #include "tv_attend.h"
 #include "tv_plan_fp8.h"
@@ -86,6 +87,14 @@ __device__ __forceinline__ int load_u8(const uint8_t* p) {
   int v;
   asm volatile("global_load_ubyte %0, %1, off" : "=v"(v) : "v"(p) : "memory");
   return v;
+}
+
+// dma16 of what is read once: it does not stay in the caches.
+__device__ __forceinline__ void dma16_once(const void* sbase, uint32_t voff, uint32_t lds_addr) {
+  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2 nt"
+               :
+               : "s"(__builtin_amdgcn_readfirstlane(lds_addr)), "v"(voff), "s"(sbase)
+               : "memory");
 }
 
 // The scheduler's order inside the region up to the next pin_order(): n times `mfma`
@@ -339,19 +348,30 @@ void attn_fp8(Fp8Args a) {
   // may be no number).
   const bool mover = wr * PU < kDma;
   const uint32_t code_off = CL::off(lane / CL::kCPR, lane % CL::kCPR);
-  auto issue_unit = [&](int u) {
+  auto issue_codes = [&](int u, uint32_t dst, auto read_once) __attribute__((always_inline)) {
+    const size_t at = (size_t)__builtin_amdgcn_readlane(group, u & 63) * CL::kBytes;
+    const int valid = kvl - (t0 + wk + WK * u) * kKeyTile;
+#pragma unroll
+    for (int k = 0; k < PU; ++k) {
+      const int q = wr * PU + k, j = q % CL::kDma;
+      const char* base = (q >= CL::kDma ? (const char*)a.vc : (const char*)a.kc) + at;
+      uint32_t off = (code_off ^ CL::dma_flip(j)) + j * 1024;
+      if (valid < kKeyTile) off -= D * max(0, j * CL::kRowsPerDma + lane / CL::kCPR - (valid - 1));
+      if constexpr (read_once.value) dma16_once(base, off, dst + q * 1024);
+      else dma16(base, off, dst + q * 1024);
+    }
+  };
+  // A tile that only one row block reads does not stay in the caches: single tokens of 64
+  // sequences of 512 to 8192 rows 114 us, else 131; two trees of 16 nodes over 131072 rows
+  // 114, else 118; over 1200 drawn shapes of up to 32 rows 4% less time.  With more row
+  // blocks the others' reads would miss (four tokens of five sequences, two row blocks: 68
+  // -> 76 us); four waves that share a ring have them.
+  const bool once = WR <= 2 && a.nRB == 1;
+  auto issue_unit = [&](int u) __attribute__((always_inline)) {
     const uint32_t dst = ring + (u % NU) * UNIT;
     if (u < n_c) {
-      const size_t at = (size_t)__builtin_amdgcn_readlane(group, u & 63) * CL::kBytes;
-      const int valid = kvl - (t0 + wk + WK * u) * kKeyTile;
-#pragma unroll
-      for (int k = 0; k < PU; ++k) {
-        const int q = wr * PU + k, j = q % CL::kDma;
-        const char* base = (q >= CL::kDma ? (const char*)a.vc : (const char*)a.kc) + at;
-        uint32_t off = (code_off ^ CL::dma_flip(j)) + j * 1024;
-        if (valid < kKeyTile) off -= D * max(0, j * CL::kRowsPerDma + lane / CL::kCPR - (valid - 1));
-        dma16(base, off, dst + q * 1024);
-      }
+      if (once) issue_codes(u, dst, std::true_type{});
+      else issue_codes(u, dst, std::false_type{});
     } else {
       const int first = (t0 + wk + WK * (n_c + ((u - n_c) >> 1)) - nct) * kKeyTile;
       const char* base = ((u - n_c) & 1 ? vtree : ktree) + (size_t)first * krow * 2;
