@@ -74,8 +74,8 @@ inline bool attn_plan_fp8_fits(const AttnPlan& p) {
 // can ask for), the tree and the partials.  The constants are fitted together to 294
 // shapes drawn over the ranges of 1 to 64 sequences, 1 to 512 nodes, up to 131072 rows
 // and the heads above, each in all arrangements and up to 14 splits and merges, those of
-// the merge by a second kernel to 6000 times of both merges.  The plan picked is 2.1%
-// slower than the fastest on average on 1400 shapes that the fit has not seen (row blocks
+// the merge by a second kernel to 6000 times of both merges.  The plan picked is 2.3%
+// slower than the fastest on average on 1800 shapes that the fit has not seen (row blocks
 // as large as the tree fills, split to fill the GPU once: 18%).
 constexpr double kFp8Fill = 0.703;  // mean length of several sequences over the capacity
 constexpr double kFp8Full[] = {1.04, 0, 1.598, 1.582, 1.414, 1.202, 0.911};  // 8 waves at work
