@@ -408,7 +408,7 @@ unsigned long long tv_capture_id(hipStream_t stream) {
     (void)hipGetLastError();  // (the null stream while another thread captures)
     return 0;
   }
-  return status == hipStreamCaptureStatusActive ? id : 0;
+  return status == hipStreamCaptureStatusActive ? id + 1 : 0;  // (whatever the first id is)
 }
 
 // The page calls' common arguments; block_size 0 where the call has none.

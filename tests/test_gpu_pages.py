@@ -107,6 +107,32 @@ def test_fork(case, short):
     assert len(empty) == 0 or ok.any() or case < 3
 
 
+@pytest.mark.parametrize("nb", [8192, 30011, 65537])
+def test_pages_far_apart(nb):
+    """A pool whose counts take several passes, most of them without a free page: the first, the last
+    and the ones about a pass's end."""
+    left = np.array(sorted({0, 8190, 8191, 8192, 8193, nb - 2, nb - 1} & set(range(nb))))
+    ref = np.ones(nb, np.int64)
+    ref[left] = 0
+    B, mb, bs = 12, 4, 32
+    for short in (0, 3):
+        bt, kv = np.full((B, mb), -1, np.int64), np.zeros(B, np.int64)
+        n = np.zeros(B, np.int64)
+        n[:len(left) + short] = 5
+        ok, et, er = ref_pages.reserve(n, bt, kv, ref, bs)
+        dt, dk, dr = dev_i32(bt), dev_i32(kv), dev_i32(ref)
+        got = reserve_pages(dev_i32(n), dt, dk, dr, bs)
+        assert eq(got, ok) and eq(dt, et) and eq(dr, er) and ok.sum() == len(left) + B - min(B, len(left) + short)
+        # forks of a row with one partly filled page
+        bt[0, 0], kv[0] = 5, 7
+        src, dst = np.zeros(len(left) + short, np.int64), np.arange(1, len(left) + short + 1)
+        want = ref_pages.fork(src, dst, bt, kv, ref, bs)
+        dt, dk, dr = dev_i32(bt), dev_i32(kv), dev_i32(ref)
+        got = fork_pages(dev_i32(src), dev_i32(dst), dt, dk, dr, bs)
+        assert all(eq(x, y) for x, y in zip(list(got) + [dt, dk, dr], want))
+        assert want[0].sum() == len(left)
+
+
 @pytest.mark.parametrize("case", range(len(SHAPES)))
 def test_free(case):
     B, mb, nb, bs, fill = SHAPES[case]
