@@ -489,7 +489,11 @@ void attn_fp8(Fp8Args a) {
   const bool busy = wrow0 < a.M;  // else only the tiles are moved
   uint32_t bits[NT] = {};
   int head = 0;  // units taken so far
-  auto refill = [&]() {  // in the place of the units before `head`
+  // Fills the places of the units before `head` again.  Their LDS reads must be done by
+  // then: behind a shared ring's barrier they are, and a wave alone waits for its own
+  // (that their values were used earlier does not order the reads before the DMAs).
+  auto refill = [&]() {
+    if (kAlone) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     while (issued < n_units && issued < head + NU) {
       if (issued < n_c && (issued & 63) == 0) {
         group = group_of(issued);
@@ -525,7 +529,6 @@ void attn_fp8(Fp8Args a) {
     read_keys<D>(unit, codes, hg4, hl16);
     if (kAlone) {
       read_values<D>(unit, codes, hg4, hl16);
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       refill();
     }
   };
