@@ -313,6 +313,8 @@ void attn_main(AttnArgs a) {
         issue_tile<D, PW, kPaged>(src, dma_off, wr, lane, t0 + wk + WK * (i + NS - 1),
                           ring + ((i + NS - 1) % NS) * STAGE);
     } else {
+      // a wave by itself: its LDS reads of tile i-1, whose stage the DMAs take
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       if (i + NS - 1 < n_mine)
         issue_tile<D, PW, kPaged>(src, dma_off, wr, lane, t0 + wk + WK * (i + NS - 1),
                           ring + ((i + NS - 1) % NS) * STAGE);

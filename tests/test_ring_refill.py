@@ -20,3 +20,11 @@ def test_8_bit_ring():
     assert re.match(rf"\s*if \(kAlone\) {WAIT}", refill)
     # units are issued there and, into an empty ring, by the prologue
     assert len(re.findall(r"issue_unit\((?!int)", body)) == 2 and "issue_unit(issued)" in refill
+
+
+def test_16_bit_ring():
+    body = source("tv_attention.hip")
+    step = re.search(r"auto ring_step = \[&\]\(int i\) \{(.*?)\n  \};", body, re.S).group(1)
+    shared, alone = re.split(r"\} else \{", step)
+    assert "__syncthreads();" in shared.partition("issue_tile")[0]
+    assert re.match(rf"\s*{WAIT}", alone) and "issue_tile" in alone
