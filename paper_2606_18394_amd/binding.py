@@ -315,7 +315,8 @@ def _capture_workspace(capture: int, nbytes: int, device, stream_ptr: int) -> to
     """The attention's workspace of the calls that graph capture `capture` records
     on a stream.  It lies in the graph's own memory and is cleared by the graph:
     graphs captured on one stream may be replayed at the same time, and beside
-    eager calls on that stream."""
+    eager calls on that stream.  (The last capture's stays referenced here until
+    the stream's next one, also after its graph is gone.)"""
     key = (_device_name(device), stream_ptr)
     last, ws = _captures.get(key, (0, None))
     if last != capture or ws.numel() < nbytes:
@@ -327,10 +328,13 @@ def _capture_workspace(capture: int, nbytes: int, device, stream_ptr: int) -> to
 
 
 def _attention_workspace(nbytes: int, device, stream_ptr: int) -> torch.Tensor:
+    """The 8-bit cache's attention's: a capture's own, or the stream's.  The
+    latter is not the one of the 16-bit calls, which a graph captured with them
+    keeps using on whichever stream it is replayed."""
     capture = load_library().tv_capture_id(stream_ptr)
     if capture:
         return _capture_workspace(capture, nbytes, device, stream_ptr)
-    return workspace("attn", nbytes, device, stream_ptr)
+    return workspace("attn_fp8", nbytes, device, stream_ptr)
 
 
 _BF16, _F8, _U8, _I32 = torch.bfloat16, torch.float8_e4m3fn, torch.uint8, torch.int32
@@ -377,8 +381,9 @@ def tree_verify_attention_paged_fp8(q, k_pool, v_pool, k_exp, v_exp, block_table
     block_size // 32] uint8; block_table [B, max_blocks] int32; q, k_tree,
     v_tree, out bf16 as in tree_verify_attention (no tree-tail layout);
     parent [B, N] int32, or None for a chain (N = 1: single-token decoding).
-    Without workspace_tensor (zeros before its first use) a stream's calls share
-    one, and the calls of a graph capture have one of their own.
+    Without workspace_tensor (zeros before its first use) a stream's calls of
+    this function share one, and the calls of a graph capture have one of their
+    own.
     """
     if _direct is not None:
         done = _direct.attention(q, k_pool, v_pool, k_exp, v_exp, block_table, k_tree, v_tree, parent,

@@ -172,7 +172,7 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     PyObject* own = nullptr;
     if (ws == Py_None) {
       const unsigned long long capture = lib.capture_id(stream);
-      PyObject* args[4] = {capture ? PyLong_FromUnsignedLongLong(capture) : PyUnicode_FromString("attn"),
+      PyObject* args[4] = {capture ? PyLong_FromUnsignedLongLong(capture) : PyUnicode_FromString("attn_fp8"),
                            PyLong_FromSize_t(need), PyObject_GetAttrString(a[0], "device"),
                            PyLong_FromVoidPtr(stream)};
       ws = own = PyObject_Vectorcall(capture ? capture_workspace : workspace, args, 4, nullptr);

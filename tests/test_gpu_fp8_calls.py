@@ -311,3 +311,56 @@ def test_far_pages():
     # and through the page calls
     tv.copy_pages(dev_i32([nb - 2]), dev_i32([nb - 3]), [k, v, ke, ve])
     assert torch.equal(v[nb - 3].view(torch.uint8), v[5].view(torch.uint8))
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_beside_a_graph_of_the_16_bit_call(native, monkeypatch):
+    """A graph captured with the 16-bit call, which keeps its stream's workspace, replayed on another
+    stream while that stream makes eager 8-bit calls: both split, neither sees the other's partials."""
+    if native:
+        binding.load_library()
+        assert binding._direct is not None
+    else:
+        monkeypatch.setattr(binding, "_direct", None)
+    args, kv = attention_args(10)
+    q, table, kt, vt, parent, out = args[0], args[5], args[6], args[7], args[8], args[9]
+    B, N, Hq, D = q.shape
+    nb, Hkv, bs, _ = args[1].shape
+    g = torch.Generator(device="cuda")
+    g.manual_seed(4)
+    pools = [torch.randn(nb, bs, Hkv, D, generator=g, device="cuda").to(torch.bfloat16) for _ in range(2)]
+    lib = binding.load_library()
+    sizes = (B, N, Hq, Hkv, D, table.shape[1] * bs)
+    assert lib.tv_tree_verify_attention_workspace(*sizes) > 1 << 15
+    assert lib.tv_tree_verify_attention_paged_fp8_workspace(*sizes) > 1 << 15
+    wide = torch.empty_like(out)
+
+    def bf16_call():
+        tv.tree_verify_attention_paged(q, *pools, table, kt, vt, parent, wide, kv_len=kv)
+
+    def fp8_call():
+        tv.tree_verify_attention_paged_fp8(*args, kv_len=kv)
+
+    side, other = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        bf16_call()
+        fp8_call()
+    torch.cuda.synchronize()
+    want = bits(wide), bits(out)
+    held = {key[0]: ws.data_ptr() for key, ws in binding._workspaces.items() if key[2] == side.cuda_stream}
+    assert held["attn"] != held["attn_fp8"]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        bf16_call()
+    for _ in range(4):
+        wide.zero_()
+        out.zero_()
+        torch.cuda.synchronize()
+        for _ in range(10):
+            with torch.cuda.stream(other):
+                graph.replay()
+            with torch.cuda.stream(side):
+                fp8_call()
+        torch.cuda.synchronize()
+        assert np.array_equal(bits(wide), want[0]) and np.array_equal(bits(out), want[1])
