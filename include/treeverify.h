@@ -196,9 +196,10 @@ int tv_tree_verify_attention_paged_fp8(const void* q, const void* k_pool, const 
  * largest size among its new values and e(a) the least e of [16, 247] with
  * a <= 448 * 2^(e - 127): the exponent byte becomes e(a), or, if the group
  * holds older rows of the sequence, the larger of e(a) and its byte so far;
- * new codes are the nearest to x * 2^(127 - e) (ties to even), and older
- * codes the nearest to what they stand for (so unchanged unless the byte
- * grew).  Positions behind the last row keep what they hold.  A sequence
+ * new codes are the nearest to x * 2^(127 - e) (ties to even; at e = 247, which
+ * only sizes above 1.75 * 2^127 lead to, at most 240, so that every code stands
+ * for a bf16 number), and older codes the nearest to what they stand for (so
+ * unchanged unless the byte grew).  Positions behind the last row keep what they hold.  A sequence
  * whose n_new is outside [0, T], whose kv_len is negative, or that lacks a
  * page for one of its rows (it would pass its max_blocks pages, or an entry of
  * its block_table is outside [0, num_blocks)) is left unchanged: pools,

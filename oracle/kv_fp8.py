@@ -9,7 +9,8 @@ What the writers compute, per sequence, touched group of 32 positions, head, and
   a    the largest size among the group's new values
   e(a) the least e of [16, 247] with a <= 448 * 2^(e - 127)
   e'   max(e(a), the group's byte) if the group holds older rows of the sequence, else e(a)
-  new codes      nearest(value * 2^(127 - e'))
+  new codes      nearest(value * 2^(127 - e')), where e' = 247 of sizes up to 240: the next code
+                 would stand for 2^128, which a bf16 number does not reach
   older codes    nearest(value(code) * 2^(byte - e')), unchanged where e' is the byte
 
 nearest: to the nearest e4m3 value, ties to the even code, 448 at most.
@@ -45,6 +46,12 @@ def nearest(x):
     return (code + 128 * np.signbit(x)).astype(np.uint8)
 
 
+def codes_at(x, e):
+    """Codes of the numbers x at exponents e (of x's shape, or to be broadcast to it)."""
+    limit = np.where(np.asarray(e) == EMAX, 240.0, 448.0)
+    return nearest(np.clip(x * np.exp2(127.0 - e), -limit, limit))
+
+
 def decode(codes, exps):
     """Codes [..., rows, D] and exponents [..., rows / 32] -> the numbers they stand for."""
     scale = np.exp2(np.repeat(np.asarray(exps, np.float64) - 127, GROUP, axis=-1))
@@ -56,7 +63,7 @@ def encode(x):
     x = np.asarray(x, np.float64)
     g = x.reshape(x.shape[:-2] + (-1, GROUP, x.shape[-1]))
     e = exponent(np.abs(g).max((-1, -2)))
-    return nearest(g * np.exp2(127.0 - e)[..., None, None]).reshape(x.shape), e.astype(np.uint8)
+    return codes_at(g, e[..., None, None]).reshape(x.shape), e.astype(np.uint8)
 
 
 def exponent(a):
@@ -91,7 +98,7 @@ def append(pool, exps, table, kv_len, new, n_new):
                 e = np.maximum(e, was)
                 v = VALUES[pool[page, :, row:row + old]] * np.exp2((was - e).astype(float))[:, None, None]
                 pool[page, :, row:row + old] = nearest(v)
-            pool[page, :, row + old:row + hi] = nearest(val * np.exp2(127.0 - e)[:, None, None])
+            pool[page, :, row + old:row + hi] = codes_at(val, e[:, None, None])
             exps[page, :, row // GROUP] = e
     return pool, exps
 

@@ -6,8 +6,8 @@
 //   a   the largest size among the group's new values
 //   e   the least byte of [16, 247] with a <= 448 * 2^(e - 127); if the group holds older
 //       rows of the sequence, at least its byte so far
-//   new codes: the nearest to x * 2^(127 - e); older codes: the nearest to what they stand
-//   for at the new exponent, so unchanged unless it grew
+//   new codes: the nearest to x * 2^(127 - e), 240 at most where e is 247; older codes: the
+//   nearest to what they stand for at the new exponent, so unchanged unless it grew
 // Powers of two make every step but the one rounding exact, and older codes lose nothing
 // but what falls below the smallest code.
 //
@@ -81,6 +81,14 @@ __device__ __forceinline__ int two_codes(int w, float scale, int into) {
                                          __int_as_float(w & 0xFFFF0000) * scale, into, kHigh);
 }
 
+// At the largest exponent code 0x78 would stand for 2^128, which neither bf16 nor fp32
+// holds (the largest numbers, scaled, are below 256 and may round to it): such codes
+// become 0x77, 240.
+__device__ __forceinline__ int limited(int w) {
+  const int ones = w >> 3 & w >> 4 & w >> 5 & w >> 6, rest = w | w >> 1 | w >> 2;
+  return w - (ones & ~rest & 0x01010101);
+}
+
 // Four codes at another exponent.
 __device__ __forceinline__ int rescaled(int w, float scale) {
   const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
@@ -139,6 +147,7 @@ __device__ __forceinline__ void write_unit(const WriteArgs& a, int b, int kv, co
 #pragma unroll
       for (int w = 0; w < 2; ++w)
         c[w] = two_codes<true>(v[k][2 * w + 1], scale, two_codes<false>(v[k][2 * w], scale, 0));
+      if (e == kExpMax) c = i32x2{limited(c[0]), limited(c[1])};
       if (kMany) __builtin_nontemporal_store(c, (i32x2*)(out + r * D));
       else *(i32x2*)(out + r * D) = c;
     } else if (older && j < 0 && e > was) {

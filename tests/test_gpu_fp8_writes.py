@@ -183,3 +183,35 @@ def test_many_pages_are_all_looked_at():
     append_paged_fp8(dev_bf16(new[0]), dev_bf16(new[1]), *dev[:4], dev_i32(bt), dev[4])
     expect = [kv_fp8.append(codes[i], exps[i], bt, kvl, oracle.decode_bf16(new[i]), [T, 0]) for i in range(2)]
     check(codes, exps, bt, kvl, expect, kvl + np.array([T, 0]), dev)
+
+
+@pytest.mark.parametrize("T,Hkv", [(16, 1), (40, 2), (300, 8)])
+def test_the_largest_numbers(T, Hkv):
+    """Rows with the largest bf16 numbers of both signs, some of them behind older rows: codes that
+    stand for bf16 numbers, and an attention over them that gives numbers."""
+    from paper_2606_18394_amd import tree_verify_attention_paged_fp8
+    rng = np.random.default_rng(T)
+    B, D, bs, mb = 3, 64, 64, 8
+    bt, nb = synth.block_table(rng, B, mb)
+    kvl = np.array([0, 40, 63], np.int32)
+    codes, exps = pools(rng, nb, Hkv, bs, D)
+    new = [values(rng, (B, T, Hkv, D)) for _ in range(2)]
+    # anywhere among the keys; among the values once per column, so that a sum of theirs stays finite
+    for x, huge in zip(new, (rng.random(new[0].shape) < 0.05,
+                             np.arange(T)[:, None, None] == rng.integers(0, T, size=(B, 1, Hkv, D)))):
+        x[huge] = 0x7F60 + rng.integers(0, 32, size=huge.sum()) | rng.integers(0, 2, size=huge.sum()) << 15
+    dev = [dev_f8(codes[0]), dev_f8(codes[1]), dev_u8(exps[0]), dev_u8(exps[1]), dev_i32(kvl)]
+    append_paged_fp8(dev_bf16(new[0]), dev_bf16(new[1]), *dev[:4], dev_i32(bt), dev[4])
+    expect = [kv_fp8.append(codes[i], exps[i], bt, kvl, oracle.decode_bf16(new[i]), [T] * B) for i in range(2)]
+    check(codes, exps, bt, kvl, expect, kvl + T, dev)
+    assert (expect[1][1] == 247).any()
+    for c, e in expect:   # (codes behind a sequence's last row are not its)
+        rows = kv_fp8.gather(c, e, bt, mb)
+        for b in range(B):
+            assert np.isfinite(rows[b, :kvl[b] + T].astype(np.float32)).all()
+    # queries of zeros: every score is 0, and the output the mean of the values
+    q = torch.zeros(B, 1, 2 * Hkv, D, dtype=torch.bfloat16, device="cuda")
+    one = torch.zeros(B, 1, Hkv, D, dtype=torch.bfloat16, device="cuda")
+    out = torch.empty_like(q)
+    tree_verify_attention_paged_fp8(q, *dev[:4], dev_i32(bt), one, one, None, out, kv_len=dev[4])
+    assert bool(torch.isfinite(out).all())

@@ -179,3 +179,23 @@ def test_page_calls_keep_their_books(seed):
         consistent(table, ref, kv, bs)
         for b in range(B):
             assert read(b) == seqs[b]
+
+
+def test_the_largest_numbers_stay_numbers():
+    """At the largest exponent a code still stands for a number that bf16 and fp32 hold: the largest
+    one of those, 240 * 2^120, for all sizes above 232 * 2^120 (halfway between codes 224 and 240; the
+    even one is 224)."""
+    bits = np.arange(0x7F60, 0x7F80, dtype=np.uint16)
+    x = oracle.decode_bf16(np.concatenate([bits, bits | 0x8000])).reshape(1, 1, 64, 1).repeat(64, -1)
+    codes, exps = kv_fp8.encode(x)
+    back = kv_fp8.decode(codes, exps)
+    assert (exps == 247).all() and np.isfinite(back.astype(np.float32)).all()
+    assert (back.astype(np.float32).view(np.uint32) & 0xFFFF == 0).all()
+    size = np.abs(x)
+    assert (np.abs(back)[size > 232 * 2.0 ** 120] == 240 * 2.0 ** 120).all()
+    assert (np.abs(back - x) <= 2.0 ** -4 * size).all() and (np.sign(back) == np.sign(x)).all()
+    # rows in a cache whose exponents are smaller: older codes halve at least, so they fit as well
+    pool, e = np.full((1, 1, 32, 64), 0x7E, np.uint8), np.full((1, 1, 1), 246, np.uint8)
+    pool, e = kv_fp8.append(pool, e, np.zeros((1, 1), int), [16], x[:, :, 16:32].transpose(0, 2, 1, 3), [16])
+    assert e[0, 0, 0] == 247 and (kv_fp8.VALUES[pool[0, 0, :16]] == 224).all()
+    assert (np.abs(kv_fp8.VALUES[pool]) <= 240).all()
