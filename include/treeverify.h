@@ -189,7 +189,9 @@ int tv_tree_verify_attention_paged_fp8(const void* q, const void* k_pool, const 
  * Appends rows to the 8-bit cache: rows 0 .. n_new[b] - 1 of sequence b (NULL
  * n_new: T) go to positions kv_len[b] .. and kv_len[b] grows by n_new[b].
  *
- *   k_new, v_new [B, T, Hkv, D] bf16, finite where used
+ *   k_new, v_new [B, T, Hkv, D] bf16, finite where used (an infinity or NaN
+ *                becomes a code that is no number, and leaves its group's
+ *                exponent and other codes what they are without it)
  *   n_new        [B] int32, in [0, T]
  *
  * Per group of 32 positions that gets rows, head, and K or V, with a the

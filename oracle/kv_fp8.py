@@ -6,14 +6,15 @@ exponent byte e per 32 positions of a page and head; a code c stands for value(c
 
 What the writers compute, per sequence, touched group of 32 positions, head, and K or V:
 
-  a    the largest size among the group's new values
+  a    the largest size among the group's new values (of those that are finite)
   e(a) the least e of [16, 247] with a <= 448 * 2^(e - 127)
   e'   max(e(a), the group's byte) if the group holds older rows of the sequence, else e(a)
   new codes      nearest(value * 2^(127 - e')), where e' = 247 of sizes up to 240: the next code
                  would stand for 2^128, which a bf16 number does not reach
   older codes    nearest(value(code) * 2^(byte - e')), unchanged where e' is the byte
 
-nearest: to the nearest e4m3 value, ties to the even code, 448 at most.
+nearest: to the nearest e4m3 value, ties to the even code, 448 at most.  An infinity or NaN becomes
+code 0x7F or 0xFF.
 """
 from __future__ import annotations
 
@@ -49,7 +50,12 @@ def nearest(x):
 def codes_at(x, e):
     """Codes of the numbers x at exponents e (of x's shape, or to be broadcast to it)."""
     limit = np.where(np.asarray(e) == EMAX, 240.0, 448.0)
-    return nearest(np.clip(x * np.exp2(127.0 - e), -limit, limit))
+    c = nearest(np.clip(_finite(x) * np.exp2(127.0 - e), -limit, limit))
+    return np.where(np.isfinite(x), c, 0x7F + 128 * np.signbit(x)).astype(np.uint8)
+
+
+def _finite(x):
+    return np.where(np.isfinite(x), x, 0.0)
 
 
 def decode(codes, exps):
@@ -62,7 +68,7 @@ def encode(x):
     """x [..., rows, D], rows a multiple of 32 -> (codes, exponents)."""
     x = np.asarray(x, np.float64)
     g = x.reshape(x.shape[:-2] + (-1, GROUP, x.shape[-1]))
-    e = exponent(np.abs(g).max((-1, -2)))
+    e = exponent(np.abs(_finite(g)).max((-1, -2)))
     return codes_at(g, e[..., None, None]).reshape(x.shape), e.astype(np.uint8)
 
 
@@ -92,7 +98,7 @@ def append(pool, exps, table, kv_len, new, n_new):
             old = max(0, kv - lo)                                  # older rows of the group
             hi = min(lo + GROUP, kv + n) - lo
             val = np.asarray(new[b, lo + old - kv:lo + hi - kv], np.float64).transpose(1, 0, 2)
-            e = exponent(np.abs(val).max((1, 2)))
+            e = exponent(np.abs(_finite(val)).max((1, 2)))
             if old:
                 was = exps[page, :, row // GROUP].astype(np.int64)
                 e = np.maximum(e, was)

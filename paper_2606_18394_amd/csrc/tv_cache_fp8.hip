@@ -3,7 +3,8 @@
 // kv_len rows, and kv_len grows.
 //
 // Per sequence, group of 32 positions that gets rows, head, and K or V:
-//   a   the largest size among the group's new values
+//   a   the largest size among the group's new values that are finite numbers (the others
+//       become codes that are no numbers, and cost their group nothing else)
 //   e   the least byte of [16, 247] with a <= 448 * 2^(e - 127); if the group holds older
 //       rows of the sequence, at least its byte so far
 //   new codes: the nearest to x * 2^(127 - e), 240 at most where e is 247; older codes: the
@@ -24,6 +25,7 @@
 namespace tv {
 
 constexpr int kGroup = 32, kExpMin = 16, kExpMax = 247;
+constexpr int kInfBits = 0x7F80;  // bf16 sizes from here on are no finite numbers
 
 struct WriteArgs {
   const __bf16* x[2];  // K's and V's rows, [B, T, Hkv, D]
@@ -40,6 +42,7 @@ struct WriteArgs {
 typedef int i32x2 __attribute__((ext_vector_type(2)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+typedef int16_t i16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 // What sequence b gets: n rows, 0 where it is left as it is; but that it has a page for
@@ -107,7 +110,6 @@ __device__ __forceinline__ void write_unit(const WriteArgs& a, int b, int kv, co
   const int first = ((kv >> 5) + gi) * kGroup, n = rows.n;  // the group's first position
   if (first >= kv + n) return;
   i32x4 v[kLoads];
-  u16x2 most = {0, 0};
 #pragma unroll
   for (int k = 0; k < kLoads; ++k) {
     const int j = first + k * kRows + lane / kLanes - kv;  // new row
@@ -127,12 +129,22 @@ __device__ __forceinline__ void write_unit(const WriteArgs& a, int b, int kv, co
   const size_t group = (((size_t)blk * a.Hkv + h) << per) + ((first >> 5) & ((1 << per) - 1));
   const bool older = first < kv;
   const int was = older ? a.exps[isv][group] : 0;
+  // the largest of the bit patterns + margin, as signed numbers, less margin (sizes: 0x7FFF
+  // twice, opaque so that what a second look needs is not kept from the first)
+  auto largest = [&](uint16_t margin) {
+    int sizes = 0x7FFF7FFF;
+    asm volatile("" : "+s"(sizes));
+    i16x2 most = {0, 0};
 #pragma unroll
-  for (int k = 0; k < kLoads; ++k)
+    for (int k = 0; k < kLoads; ++k)
 #pragma unroll
-    for (int w = 0; w < 4; ++w)
-      most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, v[k][w] & 0x7FFF7FFF));
-  const int a_bits = (int)wave_max_u32(most[0] > most[1] ? most[0] : most[1]);
+      for (int w = 0; w < 4; ++w)
+        most = __builtin_elementwise_max(
+            most, __builtin_bit_cast(i16x2, __builtin_bit_cast(u16x2, v[k][w] & sizes) + margin));
+    return max(0, (int)wave_max_u32(most[0] > most[1] ? most[0] : most[1]) - margin);
+  };
+  int a_bits = largest(0);
+  if (a_bits >= kInfBits) a_bits = largest(0x8000 - kInfBits);  // which those are negative with
   // 448 = 1.75 * 2^8: the exponent 8 below the value's, one more above 1.75
   int e = (a_bits >> 7) - 8 + ((a_bits & 127) > 96);
   e = e < kExpMin ? kExpMin : (e > kExpMax ? kExpMax : e);

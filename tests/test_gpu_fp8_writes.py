@@ -215,3 +215,30 @@ def test_the_largest_numbers(T, Hkv):
     out = torch.empty_like(q)
     tree_verify_attention_paged_fp8(q, *dev[:4], dev_i32(bt), one, one, None, out, kv_len=dev[4])
     assert bool(torch.isfinite(out).all())
+
+
+@pytest.mark.parametrize("T,Hkv,D", [(1, 2, 64), (20, 3, 128), (300, 8, 128)])
+def test_what_is_no_number_costs_its_group_nothing_else(T, Hkv, D):
+    """Infinities and NaN among the rows: codes that are no numbers there, and everything else,
+    exponents and older rows too, as without them."""
+    rng = np.random.default_rng(100 + T)
+    B, bs, mb = 3, 32, 12
+    bt, nb = synth.block_table(rng, B, mb)
+    kvl = np.array([0, 20, 63], np.int32)
+    codes, exps = pools(rng, nb, Hkv, bs, D)
+    new = [values(rng, (B, T, Hkv, D)) for _ in range(2)]
+    for x in new:
+        odd = rng.random(x.shape) < 0.01
+        odd[:, 0, :, 3] = True
+        x[odd] = rng.choice(np.array([0x7F80, 0xFF80, 0x7FC0, 0xFFC1, 0x7FFF, 0x7F81], np.uint16), odd.sum())
+    new[0][:, -1, 0] = 0x7F80                            # a whole row
+    dev = [dev_f8(codes[0]), dev_f8(codes[1]), dev_u8(exps[0]), dev_u8(exps[1]), dev_i32(kvl)]
+    append_paged_fp8(dev_bf16(new[0]), dev_bf16(new[1]), *dev[:4], dev_i32(bt), dev[4])
+    expect = [kv_fp8.append(codes[i], exps[i], bt, kvl, oracle.decode_bf16(new[i]), [T] * B) for i in range(2)]
+    for i in range(2):
+        assert ((expect[i][0] & 0x7F) == 0x7F).any() and expect[i][1].max() < 247
+        got = dev[i].view(torch.uint8).cpu().numpy()
+        no = (expect[i][0] & 0x7F) == 0x7F
+        assert ((got[no] & 0x7F) == 0x7F).all() and np.array_equal(got[~no], expect[i][0][~no])
+        assert np.array_equal(dev[2 + i].cpu().numpy(), expect[i][1])
+    assert np.array_equal(dev[4].cpu().numpy(), kvl + T)

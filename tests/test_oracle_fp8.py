@@ -199,3 +199,22 @@ def test_the_largest_numbers_stay_numbers():
     pool, e = kv_fp8.append(pool, e, np.zeros((1, 1), int), [16], x[:, :, 16:32].transpose(0, 2, 1, 3), [16])
     assert e[0, 0, 0] == 247 and (kv_fp8.VALUES[pool[0, 0, :16]] == 224).all()
     assert (np.abs(kv_fp8.VALUES[pool]) <= 240).all()
+
+
+def test_what_is_no_number_costs_its_group_nothing_else():
+    rng = np.random.default_rng(6)
+    pool, exps = rng.integers(0, 127, (2, 1, 32, 64)).astype(np.uint8), np.full((2, 1, 1), 120, np.uint8)
+    new = rng.standard_normal((1, 20, 1, 64))
+    bad = new.copy()
+    at = [(0, 3, 0, 5), (0, 3, 0, 6), (0, 11, 0, 7), (0, 19, 0, 63)]
+    for i, x in zip(at, (np.inf, -np.inf, np.nan, -np.nan)):
+        bad[i], new[i] = x, 0.0
+    table = np.array([[1, 0]])
+    want = kv_fp8.append(pool, exps, table, [7], new, [20])
+    got = kv_fp8.append(pool, exps, table, [7], bad, [20])
+    codes = [got[0][1, 0, 7 + i[1], i[3]] for i in at]
+    assert codes[:2] == [0x7F, 0xFF] and all(c & 0x7F == 0x7F for c in codes)
+    for i in at:
+        got[0][1, 0, 7 + i[1], i[3]] = 0
+    np.testing.assert_array_equal(got[0], want[0])
+    np.testing.assert_array_equal(got[1], want[1])
