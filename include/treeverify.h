@@ -268,8 +268,9 @@ int tv_reserve_pages(const int32_t* n_rows, int32_t* block_table, const int32_t*
  * it are copied to; kv_len[dst[i]] = kv_len[src[i]].  Pages that src[i] has
  * beyond kv_len are not shared.  ok[i] = 1, or 0 where nothing is done: src[i]
  * or dst[i] outside [0, B), row dst[i] not empty, dst[i] named by an earlier
- * fork, src[i] the dst of any fork, or no page left for the copy (in the order
- * of i).  copy_src, copy_dst [n]: the pages copied, -1 where none. */
+ * fork, src[i] the dst of any fork, src[i] without a page for one of its rows
+ * (an entry outside [0, num_blocks)), or no page left for the copy (in the
+ * order of i).  copy_src, copy_dst [n]: the pages copied, -1 where none. */
 int tv_fork_pages(const int32_t* src, const int32_t* dst, int n, int32_t* block_table, int32_t* kv_len,
                   int32_t* ref_count, int B, int max_blocks, int block_size, int num_blocks,
                   void* const* pools, const int64_t* page_bytes, int n_pools, int32_t* ok,

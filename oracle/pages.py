@@ -51,6 +51,9 @@ def fork(src, dst, table, kv_len, ref, block_size):
         if not 0 <= kv[s] <= mb * block_size:
             continue
         full, part = divmod(int(kv[s]), block_size)
+        mine = before[s, :full + (part > 0)]
+        if ((mine < 0) | (mine >= len(ref))).any():
+            continue
         if part:
             taken += 1
             if taken > len(free):

@@ -541,8 +541,9 @@ def fork_pages(src, dst, block_table, kv_len, ref_count, block_size, pools=(), o
     """Sequence dst[i] (an empty row) continues sequence src[i] (int32 [n]): it
     shares src's full pages, and its last, partly filled page is copied in all
     `pools` ([num_blocks, ...] tensors).  Returns (ok, copy_src, copy_dst) int32
-    [n]: whether the fork was made, and the pages copied (-1: none), for
-    copy_pages on further pools."""
+    [n]: whether the fork was made (not if src lacks a page for one of its rows,
+    dst's row is not empty, or no page is left for the copy), and the pages
+    copied (-1: none), for copy_pages on further pools."""
     pools = tuple(pools)
     if _direct is not None and ok is None and copy_src is None and copy_dst is None:
         done = _direct.fork(src, dst, block_table, kv_len, ref_count, block_size, pools)

@@ -189,3 +189,33 @@ def test_compact(nb, share):
     got = compact_pages(dt, dr, pools)
     assert int(got[0]) == live and eq(got[1], cs) and eq(got[2], cd)
     assert eq(dt, et) and eq(dr, er) and same(pools, want)
+
+
+@pytest.mark.parametrize("case", range(1, len(SHAPES)))
+def test_fork_of_rows_that_lack_a_page(case):
+    """Sources whose kv_len covers an entry that is no page (the partly filled one, any other, a
+    number outside the pool) are not forked, take no page and leave the others' pages theirs."""
+    B, mb, nb, bs, fill = SHAPES[case]
+    nb = min(nb, 20000)
+    rng = np.random.default_rng(5500 + case)
+    bt, kv, ref = state(rng, B, mb, nb, bs, fill * 0.8)
+    empty, rows = np.flatnonzero(bt[:, 0] < 0), np.flatnonzero(kv > 0)
+    if len(empty) == 0 and len(rows) > 1:
+        empty, rows = rows[-1:], rows[:-1]
+        bt[empty], kv[empty] = -1, 0
+    for b in rows[rng.random(len(rows)) < 0.4]:
+        last = int(kv[b] - 1) // bs
+        j = last if rng.random() < 0.5 else int(rng.integers(0, mb))     # (behind the rows: no matter)
+        bt[b, j] = rng.choice([-1, -2 ** 31, nb, 2 ** 31 - 1])
+    kv[rows[::7]] = mb * bs                                              # a length beyond the pages
+    n = min(1024, 2 * len(empty))
+    src = rng.choice(rows, size=n)
+    dst = np.concatenate([empty, empty])[:n]
+    ok, cs, cd, et, ek, er = ref_pages.fork(src, dst, bt, kv, ref, bs)
+    pools = pool_set(rng, nb)[2:5]
+    want = moved(pools, cs, cd)
+    dt, dk, dr = dev_i32(bt), dev_i32(kv), dev_i32(ref)
+    got = fork_pages(dev_i32(src), dev_i32(dst), dt, dk, dr, bs, pools)
+    assert eq(got[0], ok) and eq(got[1], cs) and eq(got[2], cd)
+    assert eq(dt, et) and eq(dk, ek) and eq(dr, er) and same(pools, want)
+    assert case < 3 or (ok.any() and not ok[:len(empty)].all())

@@ -218,3 +218,17 @@ def test_what_is_no_number_costs_its_group_nothing_else():
         got[0][1, 0, 7 + i[1], i[3]] = 0
     np.testing.assert_array_equal(got[0], want[0])
     np.testing.assert_array_equal(got[1], want[1])
+
+
+def test_a_fork_needs_every_page_of_its_source():
+    """No trace of a fork whose source lacks a page: the partly filled one, a full one, one outside
+    the pool; pages behind its rows do not matter."""
+    table = np.full((8, 4), -1)
+    table[0], table[1], table[2] = [0, 1, -1, -1], [0, -1, 2, -1], [3, 9, -1, -1]
+    table[3] = [3, 4, -1, 77]
+    kv, ref = np.array([70, 70, 64, 64, 0, 0, 0, 0]), np.array([2, 1, 1, 2, 1, 0, 0, 0])
+    src, dst = [0, 1, 2, 3], [4, 5, 6, 7]
+    ok, cs, cd, t, k, r = pages.fork(src, dst, table, kv, ref, 32)
+    assert ok.tolist() == [0, 0, 0, 1] and (cs == -1).all() and (cd == -1).all()
+    assert (t[4:7] == -1).all() and t[7].tolist() == [3, 4, -1, -1] and k[4:].tolist() == [0, 0, 0, 64]
+    assert r.tolist() == [2, 1, 1, 3, 2, 0, 0, 0]
