@@ -364,3 +364,56 @@ def test_beside_a_graph_of_the_16_bit_call(native, monkeypatch):
                 fp8_call()
         torch.cuda.synchronize()
         assert np.array_equal(bits(wide), want[0]) and np.array_equal(bits(out), want[1])
+
+
+def test_native_half_does_every_call(monkeypatch):
+    """With the Python half's checks made to raise, every call that has a native half still goes
+    through, and with the results that the Python half gives; a native half that declines does not."""
+    def steps(cache, table, kv, ref, rows, tree):
+        tv.tree_verify_attention_paged_fp8(*args, kv_len=lens)
+        yield "attention", [args[9]]
+        yield "reserve", [tv.reserve_pages(dev_i32([70, 40, 33, 5]), table, kv, ref, 32), table, ref]
+        tv.append_paged_fp8(rows, rows, *cache, table, kv, n_new=dev_i32([70, 40, 33, 0]))
+        yield "append", cache + [kv]
+        tv.commit_path_paged_fp8(tree, tree, dev_i32([[0, 2, 3]] * 4), dev_i32([3, 2, 1, -1]), *cache, table, kv)
+        yield "commit", cache + [kv]
+        tv.free_pages(dev_i32([1, 3]), table, kv, ref)
+        yield "free", [table, kv, ref]
+        said = tv.fork_pages(dev_i32([0, 2]), dev_i32([1, 3]), table, kv, ref, 32, cache)
+        yield "fork", list(said) + cache + [table, kv, ref]
+
+    def state():
+        cache, table, kv, ref, rows = serving_state(5)
+        return cache, table, kv, ref, rows(70), rows(5)
+
+    def run():
+        return [(name, [x.view(torch.uint8).cpu().clone() for x in seen]) for name, seen in steps(*state())]
+
+    args, lens = attention_args(8)
+    binding.load_library()
+    native = binding._direct
+    assert native is not None
+    monkeypatch.setattr(binding, "_direct", None)
+    want = run()
+    assert [name for name, _ in want] == ["attention", "reserve", "append", "commit", "free", "fork"]
+    monkeypatch.setattr(binding, "_direct", native)
+
+    def raises(*a, **k):
+        raise AssertionError("the Python half was asked")
+
+    monkeypatch.setattr(binding, "_need_all", raises)
+    args[9].zero_()
+    for (name, seen), (_, expect) in zip(run(), want):
+        assert all(torch.equal(x, y) for x, y in zip(seen, expect)), name
+
+    class Declines:
+        def __init__(self, name):
+            self.name = name
+
+        def __getattr__(self, name):
+            return (lambda *a: None) if name == self.name else getattr(native, name)
+
+    for name, _ in want:
+        monkeypatch.setattr(binding, "_direct", Declines(name))
+        with pytest.raises(AssertionError, match="Python half"):
+            run()
