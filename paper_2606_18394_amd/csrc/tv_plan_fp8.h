@@ -76,7 +76,11 @@ inline bool attn_plan_fp8_fits(const AttnPlan& p) {
 // and the heads above, each in all arrangements and up to 14 splits and merges, those of
 // the merge by a second kernel to 6000 times of both merges.  The plan picked is 2.3%
 // slower than the fastest on average on 1800 shapes that the fit has not seen (row blocks
-// as large as the tree fills, split to fill the GPU once: 18%).
+// as large as the tree fills, split to fill the GPU once: 18%).  As a time the cost is
+// rougher than that: all but the merge's constants were fitted before tiles that are read
+// once passed the caches by (single tokens of 64 sequences: cost 133, time 104 to 112;
+// two trees of 16 nodes over 131072 rows: 84, 115), and trees of more than 512 nodes were
+// not among the shapes.
 constexpr double kFp8Fill = 0.703;  // mean length of several sequences over the capacity
 constexpr double kFp8Full[] = {1.04, 0, 1.598, 1.582, 1.414, 1.202, 0.911};  // 8 waves at work
 static_assert(sizeof(kFp8Full) / sizeof(kFp8Full[0]) == kNumArrangementsFp8, "one per arrangement");
