@@ -101,7 +101,7 @@ __device__ __forceinline__ int rescaled(int w, float scale) {
 
 // Unit (group gi of those that get rows, head h, K or V) of sequence b with its new rows
 // from kv on.  kMany: loads and stores that do not stay in the caches (four prompts, 125 MB in
-// all: 39 us, now 32).
+// all: 39 us, now 33).
 template <int D, bool kMany>
 __device__ __forceinline__ void write_unit(const WriteArgs& a, int b, int kv, const Rows& rows, int gi, int h,
                                            int isv) {
