@@ -92,7 +92,10 @@ bool stream_of(int64_t device, void** stream) {
   return !PyErr_Occurred();
 }
 
+// What binding.py will meet and raise again is cleared; an interrupt or exit that came in
+// while a Python function was asked is not an error of the call, and goes on.
 PyObject* none() {
+  if (PyErr_Occurred() && !PyErr_ExceptionMatches(PyExc_Exception)) return nullptr;
   PyErr_Clear();
   Py_RETURN_NONE;
 }

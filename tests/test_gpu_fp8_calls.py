@@ -417,3 +417,35 @@ def test_native_half_does_every_call(monkeypatch):
         monkeypatch.setattr(binding, "_direct", Declines(name))
         with pytest.raises(AssertionError, match="Python half"):
             run()
+
+
+@pytest.mark.parametrize("error", [KeyboardInterrupt, SystemExit, ValueError])
+def test_an_interrupt_is_not_lost_in_the_native_half(error):
+    """What is raised while the native half asks for a workspace: an interrupt reaches the caller, and
+    nothing is launched; an error of the call is left to the Python half, which meets it again."""
+    args, kv = attention_args(4)
+    native = binding._direct if binding.load_library() and binding._direct is not None else None
+    assert native is not None
+
+    def ask(*a):
+        raise error("now")
+
+    def connect(workspace):
+        native.connect(binding.load_library()._handle, binding._raw_stream, torch._C._cuda_getDevice, workspace,
+                       binding._capture_workspace)
+
+    args[9].fill_(3.0)
+    connect(ask)
+    try:
+        if error is ValueError:
+            assert native.attention(*args, kv, None, None) is None
+        else:
+            with pytest.raises(error):
+                native.attention(*args, kv, None, None)
+            with pytest.raises(error):
+                tv.tree_verify_attention_paged_fp8(*args, kv_len=kv)
+    finally:
+        connect(binding.workspace)
+    torch.cuda.synchronize()
+    assert bool((args[9] == 3.0).all())
+    assert native.attention(*args, kv, None, None) is args[9]
